@@ -1,13 +1,31 @@
 """The policy update's operators as differentiable functions of torch tensors.
 
 Each wraps a forward and a backward call of ``binding``; what the backward call needs (inputs, outputs, statistics) is kept,
-logits never are.  Everything is on the current stream of the tensors' device.
+logits never are.  Everything is on the current stream of the tensors' device.  Gradients are of first order: the backward calls
+leave no history, so differentiating through a gradient raises.
 """
 from __future__ import annotations
 
 import torch
 
 from . import binding as B
+
+
+class _FirstOrder(torch.autograd.Function):
+    """Gradients as they are, with a history that ends in an error.  ``sources``: what they were computed from (torch's once_differentiable
+    looks at the incoming gradients alone: of ``f(q).sum()`` they need none, and q's part would be left out without a word)."""
+    @staticmethod
+    def forward(ctx, n, *grads_and_sources):
+        return tuple(None if g is None else g.detach() for g in grads_and_sources[:n])
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("the gradients of qk_norm_rope, packed_attn and linear_logprob are of first order: they cannot be differentiated again")
+
+
+def _first_order(grads, sources):
+    """What a backward method returns: the plain gradients, unless it runs with create_graph."""
+    return _FirstOrder.apply(len(grads), *grads, *sources) if torch.is_grad_enabled() else tuple(grads)
 
 
 class _QkNormRope(torch.autograd.Function):
@@ -20,9 +38,8 @@ class _QkNormRope(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dq_out, dk_out):
         q, k, q_weight, k_weight, positions, inv_freq = ctx.saved_tensors
-        dq, dk, dqw, dkw = B.rl_qk_norm_rope_backward(dq_out.contiguous(), dk_out.contiguous(), q, k, positions, inv_freq, ctx.sections,
-                                                      q_weight, k_weight, ctx.eps)
-        return dq, dk, dqw, dkw, None, None, None, None
+        grads = B.rl_qk_norm_rope_backward(dq_out.contiguous(), dk_out.contiguous(), q, k, positions, inv_freq, ctx.sections, q_weight, k_weight, ctx.eps)
+        return (*_first_order(grads, (dq_out, dk_out, q, k, q_weight, k_weight)), None, None, None, None)
 
 
 class _PackedAttn(torch.autograd.Function):
@@ -36,7 +53,8 @@ class _PackedAttn(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dout):
         q, k, v, out, lse, cu_seqlens = ctx.saved_tensors
-        return (*B.rl_packed_attn_backward(dout.contiguous(), q, k, v, out, lse, cu_seqlens, ctx.scale), None, None)
+        grads = B.rl_packed_attn_backward(dout.contiguous(), q, k, v, out, lse, cu_seqlens, ctx.scale)
+        return (*_first_order(grads, (dout, q, k, v)), None, None)
 
 
 class _LinearLogprob(torch.autograd.Function):
@@ -56,11 +74,11 @@ class _LinearLogprob(torch.autograd.Function):
         if g_logprob is None:
             g_logprob = torch.zeros_like(lse)
         want = [n for n, needed in zip(("dhidden", "dweight"), ctx.needs_input_grad) if needed]
-        dh, dw = B.rl_linear_logprob_backward(hidden, weight, token_ids, lse, g_logprob.contiguous(),
-                                              entropy=None if g_entropy is None else entropy,
-                                              g_entropy=None if g_entropy is None else g_entropy.contiguous(),
-                                              inv_temperature=ctx.inv_temperature, want=want)
-        return dh, dw, None, None
+        grads = B.rl_linear_logprob_backward(hidden, weight, token_ids, lse, g_logprob.contiguous(),
+                                             entropy=None if g_entropy is None else entropy,
+                                             g_entropy=None if g_entropy is None else g_entropy.contiguous(),
+                                             inv_temperature=ctx.inv_temperature, want=want)
+        return (*_first_order(grads, (g_logprob, g_entropy, hidden, weight)), None, None)
 
 
 def qk_norm_rope(q, k, q_weight, k_weight, positions, inv_freq, sections, eps=1e-6):
