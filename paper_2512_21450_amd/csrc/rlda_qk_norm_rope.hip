@@ -25,6 +25,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int NT = 256;
 constexpr int MAX_GROUPS = 1024;                            // workgroups of a backward call: rows of its workspace
+constexpr int GRID_X = 1 << 22;                             // workgroups along x of a forward call: a dimension of a grid holds fewer than 2^32 threads, and one of more runs in part
 
 struct Side {                                               // queries or keys
   const char* x; const char* dy; char* out;                 // dy: backward only
@@ -134,7 +135,9 @@ template <typename T, int D, int TB, bool PAST>
 __global__ void __launch_bounds__(NT) qk_norm_rope_kernel(const Params P) {
   constexpr int N = Vec<T>::N, LANES = D / 2 / N, ROWS = NT / LANES;
   __shared__ Shared<D, TB> S;
-  const int t0 = blockIdx.x * TB, nt = min(TB, P.T - t0), H = P.q.H + P.k.H;
+  const int blk = (int)(blockIdx.y * GRID_X + blockIdx.x);
+  if (blk >= (P.T + TB - 1) / TB) return;
+  const int t0 = blk * TB, nt = min(TB, P.T - t0), H = P.q.H + P.k.H;
   const int i0 = (threadIdx.x % LANES) * N, Hq = P.q.H;
   const Side sq = P.q, sk = P.k;
   auto at = [&](const Row& r, const char*& src, char*& dst, int& side) {
@@ -400,7 +403,9 @@ int rl_qk_norm_rope(const rl_qk_norm_rope_desc* d, void* hip_stream) {
   typedef void (*kern_t)(const Params);
   static constexpr kern_t kerns[2][2][3] = RLNR_KERNELS(qk_norm_rope_kernel);
   const int TB = tokens_per_group(d->T);
-  hipLaunchKernelGGL(kerns[d->dtype][d->d == 128][form(TB, Hq_Hkv(d) * d->T * d->d * e)], dim3((unsigned)((d->T + TB - 1) / TB)), dim3(NT), 0, static_cast<hipStream_t>(hip_stream), P);
+  const int64_t blocks = (d->T + TB - 1) / TB;
+  const dim3 grid((unsigned)(blocks < GRID_X ? blocks : GRID_X), (unsigned)((blocks + GRID_X - 1) / GRID_X));
+  hipLaunchKernelGGL(kerns[d->dtype][d->d == 128][form(TB, Hq_Hkv(d) * d->T * d->d * e)], grid, dim3(NT), 0, static_cast<hipStream_t>(hip_stream), P);
   return hipGetLastError() == hipSuccess ? 0 : -5;
 }
 
