@@ -36,6 +36,10 @@ using namespace rlda;
 constexpr float LN2 = 0.69314718055994531f, LOG2E = 1.4426950408889634f;
 constexpr float MASKED = -1e30f;                            // stands for a masked logit: a finite number, so that 0 * MASKED is 0
 
+// Workgroups along x of a launch, a multiple of 8; more go along another dimension.  A dimension of a grid holds fewer than 2^32 threads, and a launch of
+// more is accepted and runs in part.
+constexpr int GRID_X = 1 << 21;
+
 struct Shape {
   int N, V, H;
   int tiles_m, tiles_n;
@@ -44,15 +48,18 @@ struct Shape {
 // Tile of a workgroup.  Workgroups go round the 8 dies; each die gets a contiguous run of the tiles, in which 8 tiles along n
 // come before the next along m, so that the 32 workgroups of a die read few different rows at a time.
 __device__ __forceinline__ bool place(const Shape& s, int& tm, int& tn) {
-  const int total = s.tiles_m * s.tiles_n, per = (total + 7) / 8;
-  const int t = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-  if ((int)(blockIdx.x >> 3) >= per || t >= total) return false;
+  const int total = s.tiles_m * s.tiles_n, per = (total + 7) / 8, b = (int)(blockIdx.y * GRID_X + blockIdx.x);
+  const int t = (b & 7) * per + (b >> 3);
+  if (b >> 3 >= per || t >= total) return false;
   const int group = t / (8 * s.tiles_m), first = group * 8, width = min(8, s.tiles_n - first), in = t - group * 8 * s.tiles_m;
   tm = in / width;
   tn = first + in % width;
   return true;
 }
-unsigned grid_of(int tiles) { return (unsigned)((tiles + 7) / 8 * 8); }
+dim3 grid_of(int tiles) {
+  const int n = (tiles + 7) / 8 * 8;
+  return dim3(n < GRID_X ? n : GRID_X, (n + GRID_X - 1) / GRID_X);
+}
 
 // sums over the logits of a token, in base 2: m = max, s = sum 2^(z - m), t = sum 2^(z - m) (z - m)
 struct Acc { float m, s, t; };
@@ -191,7 +198,8 @@ struct BackwardParams {
 // rows of hidden states that add something, zeros for the others and up to whole k-steps in both directions
 __global__ void __launch_bounds__(256) linear_logprob_prepare_kernel(const char* hidden, int64_t hs, int N, int H, int V, int N64, int H64,
     const int32_t* ids, const float* lse, const float* entropy, const float* gl, const float* ge, char* copy, float4* token, bool twice) {
-  const int row = blockIdx.x, n = twice ? row & 31 : row;   // twice: rows n + 32 again
+  const int row = (int)(blockIdx.y * GRID_X + blockIdx.x), n = twice ? row & 31 : row;                       // twice: rows n + 32 again
+  if (row >= N64) return;
   bool live = n < N;
   if (token) {
     float g = 0.f, e = 0.f, l = -INFINITY, ent = 0.f;
@@ -301,10 +309,12 @@ __global__ void __launch_bounds__(T::THREADS, T::THREADS == 512 ? 2 : 4) linear_
 // The splits' sums, rounded.  LANES threads share the slabs of four columns, in an order of their own that never changes: many slabs are those of few
 // tokens, whose sums would else be one long chain of loads (16 tokens, 2048 columns: 115 -> 7 us).
 template <int LANES>
-__global__ void __launch_bounds__(256) linear_logprob_round_kernel(const float* sum, int splits, int64_t slab, int H, __bf16* out, int64_t stride, bool twice) {
+__global__ void __launch_bounds__(256) linear_logprob_round_kernel(const float* sum, int splits, int64_t slab, int N, int H, __bf16* out, int64_t stride, bool twice) {
   __shared__ float4 part[256];
   constexpr int COLS = 256 / LANES;
-  const int n = blockIdx.x, col = threadIdx.x % COLS, lane = threadIdx.x / COLS, h = (blockIdx.y * COLS + col) * 4;
+  const int n = (int)(blockIdx.z * GRID_X + blockIdx.x);
+  if (n >= N) return;
+  const int col = threadIdx.x % COLS, lane = threadIdx.x / COLS, h = (blockIdx.y * COLS + col) * 4;
   float4 v{0.f, 0.f, 0.f, 0.f};
   if (h < H) {
     const float* p = sum + (size_t)n * H + h;
@@ -382,8 +392,10 @@ __global__ void __launch_bounds__(T::THREADS, 2) linear_logprob_dweight_kernel(c
   else        store(std::false_type{});
 }
 
-__global__ void __launch_bounds__(256) linear_logprob_zero_kernel(__bf16* out, int64_t stride, int H) {
-  for (int h = threadIdx.x * 8; h < H; h += 2048) *reinterpret_cast<uint4*>(out + (size_t)blockIdx.x * stride + h) = make_uint4(0, 0, 0, 0);
+__global__ void __launch_bounds__(256) linear_logprob_zero_kernel(__bf16* out, int64_t stride, int V, int H) {
+  const int v = (int)(blockIdx.y * GRID_X + blockIdx.x);
+  if (v >= V) return;
+  for (int h = threadIdx.x * 8; h < H; h += 2048) *reinterpret_cast<uint4*>(out + (size_t)v * stride + h) = make_uint4(0, 0, 0, 0);
 }
 
 // ---- host side
@@ -407,7 +419,7 @@ int bm_of(Form f) { return f == BIG ? 256 : 128; }
 int bn_of(Form f) { return f == BIG ? 256 : f == MID ? 128 : f == SMALL64 ? 64 : 32; }
 
 // `KERNEL` with `lds` bytes of dynamic LDS, which a device has to be told of once
-template <auto KERNEL, typename P> hipError_t enqueue_tile(int lds, unsigned grid, int threads, hipStream_t st, const P& params) {
+template <auto KERNEL, typename P> hipError_t enqueue_tile(int lds, dim3 grid, int threads, hipStream_t st, const P& params) {
   static std::atomic<uint64_t> told{0};
   int device = 0;
   hipError_t e = hipGetDevice(&device);
@@ -418,7 +430,7 @@ template <auto KERNEL, typename P> hipError_t enqueue_tile(int lds, unsigned gri
     if (e != hipSuccess) return e;
     told.fetch_or(bit, std::memory_order_relaxed);
   }
-  hipLaunchKernelGGL(KERNEL, dim3(grid), dim3(threads), lds, st, params);
+  hipLaunchKernelGGL(KERNEL, grid, dim3(threads), lds, st, params);
   return hipGetLastError();
 }
 template <typename T> hipError_t enqueue_forward(const ForwardParams& P, hipStream_t st) {
@@ -428,13 +440,14 @@ template <typename T> hipError_t enqueue_dz(const BackwardParams& P, hipStream_t
   return enqueue_tile<linear_logprob_dz_kernel<T>>(T::LDS, grid_of(P.f.s.tiles_m * P.f.s.tiles_n), T::THREADS, st, P);
 }
 template <typename T> hipError_t enqueue_dhidden(const DhiddenParams& P, hipStream_t st) {
-  return enqueue_tile<linear_logprob_dhidden_kernel<T>>(T::LDS, (unsigned)(P.tiles_m * P.tiles_n * P.splits), T::THREADS, st, P);
+  return enqueue_tile<linear_logprob_dhidden_kernel<T>>(T::LDS, dim3(P.tiles_m * P.tiles_n * P.splits), T::THREADS, st, P);
 }
 template <typename T> hipError_t enqueue_dweight(const DweightParams& P, hipStream_t st) {
   return enqueue_tile<linear_logprob_dweight_kernel<T>>(T::LDS, grid_of(P.s.tiles_m * P.s.tiles_n), T::THREADS, st, P);
 }
 
 constexpr int64_t LIMIT = 1 << 24, STRIDE_LIMIT = 1 << 20;
+dim3 rows_grid(int n) { return dim3(n < GRID_X ? n : GRID_X, (n + GRID_X - 1) / GRID_X); }
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 int64_t up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
 bool lies(const void* p, int64_t stride, int hidden) {
@@ -530,7 +543,7 @@ int rl_linear_logprob(const rl_linear_logprob_desc* d, void* hip_stream) {
   P.k2 = d->inv_temperature * LOG2E;
   P.part = reinterpret_cast<float4*>(ws + l.part); P.zy = reinterpret_cast<float*>(ws + l.zy);
   if (H % PAD) {                                             // zeros behind the last column
-    hipLaunchKernelGGL(linear_logprob_prepare_kernel, dim3(N), dim3(256), 0, st, static_cast<const char*>(P.hidden), P.hs, N, H, V, N, (int)l.H64,
+    hipLaunchKernelGGL(linear_logprob_prepare_kernel, rows_grid(N), dim3(256), 0, st, static_cast<const char*>(P.hidden), P.hs, N, H, V, N, (int)l.H64,
                        nullptr, nullptr, nullptr, nullptr, nullptr, ws + l.copy, nullptr, false);
     P.hidden = ws + l.copy; P.hs = l.H64;
   }
@@ -555,7 +568,7 @@ int rl_linear_logprob_backward(const rl_linear_logprob_backward_desc* d, void* h
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   if (d->dweight && !lies(d->dweight, d->dweight_stride, H)) return -2;
   if (N == 0) {
-    if (d->dweight) hipLaunchKernelGGL(linear_logprob_zero_kernel, dim3(V), dim3(256), 0, st, static_cast<__bf16*>(d->dweight), d->dweight_stride, H);
+    if (d->dweight) hipLaunchKernelGGL(linear_logprob_zero_kernel, rows_grid(V), dim3(256), 0, st, static_cast<__bf16*>(d->dweight), d->dweight_stride, V, H);
     return hipGetLastError() == hipSuccess ? 0 : -5;
   }
   if (!d->hidden_states || !d->weight || !d->token_ids || !d->lse || !d->g_logprob || (d->g_entropy && !d->entropy)) return -1;
@@ -568,7 +581,7 @@ int rl_linear_logprob_backward(const rl_linear_logprob_backward_desc* d, void* h
   const int N64 = (int)l.N64;
   const bool twice = N <= 32;
   float4* const token = reinterpret_cast<float4*>(ws + l.token);
-  hipLaunchKernelGGL(linear_logprob_prepare_kernel, dim3(N64), dim3(256), 0, st, static_cast<const char*>(d->hidden_states), d->hidden_stride, N, H, V,
+  hipLaunchKernelGGL(linear_logprob_prepare_kernel, rows_grid(N64), dim3(256), 0, st, static_cast<const char*>(d->hidden_states), d->hidden_stride, N, H, V,
                      N64, (int)l.H64, d->token_ids, d->lse, d->entropy, d->g_logprob, d->g_entropy, ws + l.copy, token, twice);
   for (int v0 = 0; v0 < V; v0 += l.piece) {
     const int v1 = v0 + l.piece < V ? v0 + l.piece : V, cols = v1 - v0;
@@ -609,10 +622,11 @@ int rl_linear_logprob_backward(const rl_linear_logprob_backward_desc* d, void* h
     const float* const sum = reinterpret_cast<const float*>(ws + l.sum);
     __bf16* const out = static_cast<__bf16*>(d->dhidden);
     const int64_t slab = (int64_t)N64 * H;
+    const dim3 rows = rows_grid(N);
     if (l.splits >= 8)
-      hipLaunchKernelGGL(linear_logprob_round_kernel<16>, dim3(N, (H + 63) / 64), dim3(256), 0, st, sum, l.splits, slab, H, out, d->dhidden_stride, twice);
+      hipLaunchKernelGGL(linear_logprob_round_kernel<16>, dim3(rows.x, (H + 63) / 64, rows.y), dim3(256), 0, st, sum, l.splits, slab, N, H, out, d->dhidden_stride, twice);
     else
-      hipLaunchKernelGGL(linear_logprob_round_kernel<1>, dim3(N, (H + 1023) / 1024), dim3(256), 0, st, sum, l.splits, slab, H, out, d->dhidden_stride, twice);
+      hipLaunchKernelGGL(linear_logprob_round_kernel<1>, dim3(rows.x, (H + 1023) / 1024, rows.y), dim3(256), 0, st, sum, l.splits, slab, N, H, out, d->dhidden_stride, twice);
   }
   return hipGetLastError() == hipSuccess ? 0 : -5;
 }

@@ -1,0 +1,95 @@
+"""rl_linear_logprob and its gradient where weights are infinite or not numbers, and at the largest sizes that the header takes.
+
+Bars are those of the parity tests: logits 8 * 2^-24 sqrt(H) max_v sum |h w| + 4 * 2^-24 |lse| (entropies and log-probs twice that); gradients
+1.1 * 2^-8 (sum of |terms| + |result|) + 2 * the logits' bar * sum of |terms|.  Sums of magnitudes are taken over finite weights.
+"""
+import numpy as np
+import pytest
+
+from oracle import policy_update_ref as R
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def B():
+    import torch
+    assert torch.cuda.is_available()
+    from paper_2512_21450_amd import binding
+    return binding
+
+
+def np64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def inputs(N, H, V, seed):
+    import torch
+    g = torch.Generator().manual_seed(seed)
+    h, w = torch.randn(N, H, generator=g).bfloat16().cuda(), (torch.randn(V, H, generator=g) * (2.5 / np.sqrt(H))).bfloat16().cuda()
+    ids = torch.randint(0, V, (N,), generator=g, dtype=torch.int32).cuda()
+    return h, w, ids, torch.randn(N, generator=g).cuda(), (0.3 * torch.randn(N, generator=g)).cuda()
+
+
+def logit_bar(H, W, lse):
+    """of rows with a distribution"""
+    ok = np.isfinite(lse)
+    W = np.where(np.isfinite(W), W, 0.0)
+    return 8 * 2.0 ** -24 * np.sqrt(H.shape[1]) * (np.abs(H[ok]) @ np.abs(W).T).max() + 4 * 2.0 ** -24 * np.abs(lse[ok]).max()
+
+
+def test_more_workgroups_than_one_dimension_of_a_grid_holds(B):
+    """2^22 tokens over 2^17 + 300 of 8 columns: more than 2^32 threads of tiles.  Rows from all over against 64 bits."""
+    import torch
+    N, V, H = 1 << 22, (1 << 17) + 300, 8
+    g = torch.Generator(device="cuda").manual_seed(0)
+    h, w = (torch.randn(n, H, generator=g, device="cuda").bfloat16() for n in (N, V))
+    ids = torch.randint(0, V, (N,), generator=g, dtype=torch.int32, device="cuda")
+    got = B.rl_linear_logprob(h, w, ids)
+    at = torch.tensor([0, 1, 255, 256, N // 2, (1 << 21) + 1, N - 257, N - 1], device="cuda")
+    z = torch.stack([(w.double() * x).sum(1) for x in h[at].double()])
+    lse = torch.logsumexp(z, 1)
+    lp = z - lse[:, None]
+    bar = 8 * 2.0 ** -24 * np.sqrt(H) * float((h[at].double().abs()[:, None] * w.double().abs()).sum(-1).max()) + 4 * 2.0 ** -24 * float(lse.abs().max())
+    for name, ref, k in (("lse", lse, 1), ("logprob", lp.gather(1, ids[at].long()[:, None])[:, 0], 2), ("entropy", -(lp.exp() * lp).sum(1), 2)):
+        assert ((got[name][at].double() - ref).abs() <= k * bar + 1e-6).all(), name
+    assert torch.isfinite(got["lse"]).all() and torch.isfinite(got["entropy"]).all()
+
+
+@pytest.mark.parametrize("N", [(1 << 24) - 70, 1 << 24])
+def test_the_most_tokens(B, N):
+    """2^24 tokens over 8 of 72 columns, with gradient: rows are those of a call of some of them"""
+    import torch
+    V, H = 8, 72
+    g = torch.Generator(device="cuda").manual_seed(0)
+    h, w = (torch.randn(n, H, generator=g, device="cuda").bfloat16() for n in (N, V))
+    ids = torch.randint(0, V, (N,), generator=g, dtype=torch.int32, device="cuda")
+    gl = torch.zeros(N, device="cuda")
+    # 256 tokens, in one tile and from all over, have gradients: dweight is theirs
+    at = torch.cat([torch.arange(0, 64), torch.arange(1 << 23, (1 << 23) + 64), torch.arange(N - 128, N)]).cuda()
+    gl[at] = torch.randn(256, generator=g, device="cuda")
+    got = B.rl_linear_logprob(h, w, ids)
+    dh, dw = B.rl_linear_logprob_backward(h, w, ids, got["lse"], gl)
+    ref = B.rl_linear_logprob(h[at], w, ids[at])
+    rh, rw = B.rl_linear_logprob_backward(h[at], w, ids[at], ref["lse"], gl[at])
+    assert all(torch.equal(got[k][at], ref[k]) for k in got)
+    mag = dh[at].float().abs() + rh.float().abs()
+    assert ((dh[at].float() - rh.float()).abs() <= 2.0 ** -7 * mag).all() and dh[at].abs().max() > 0.1        # a rounding of each
+    idle = torch.ones(N, dtype=torch.bool, device="cuda")
+    idle[at] = False
+    assert (dh[idle] == 0).all()
+    z = h[at].double() @ w.double().T.contiguous()
+    dz = -z.softmax(1)
+    dz[torch.arange(256), ids[at].long()] += 1
+    dz *= gl[at].double()[:, None]
+    rw, mw = dz.T.contiguous() @ h[at].double(), dz.abs().T.contiguous() @ h[at].double().abs()
+    assert ((dw.double() - rw).abs() <= 1.1 * 2.0 ** -8 * (mw + rw.abs()) + 1e-4 * mw).all()
+
+
+def test_the_largest_vocabulary_without_tokens(B):
+    import torch
+    w = torch.ones(1 << 24, 8, dtype=torch.bfloat16, device="cuda")
+    h, ids, f = torch.zeros(0, 8, dtype=torch.bfloat16, device="cuda"), torch.zeros(0, dtype=torch.int32, device="cuda"), torch.zeros(0, device="cuda")
+    dw = torch.ones_like(w)
+    B.rl_linear_logprob_backward(h, w, ids, f, f, want=(), dweight=dw)
+    assert (dw == 0).all()
