@@ -77,7 +77,8 @@ typedef struct {
 /*
  * Both: enqueue on `hip_stream` (hipStream_t as void*; NULL = default stream), asynchronous, allocate nothing.  Return 0
  * or a negative code with the meaning of the RLDA_ERR_* values of rl_decode_attn.h: -1 invalid argument (NULL where a tensor
- * is required, negative sizes, scale not finite), -2 unsupported (dtype, d, head counts, strides or alignment, T > 2^24),
+ * is required, negative sizes, scale not finite), -2 unsupported (dtype, d, head counts, strides or alignment, T > 2^24,
+ * heads times tokens beyond a launch's 2^32 threads: T * Hq or T * Hkv from 2^29 on),
  * -3 workspace, -4 struct_size, -5 HIP error.  With T = 0 nothing is read or written.
  */
 int rl_packed_attn(const rl_packed_attn_desc* desc, void* hip_stream);

@@ -111,6 +111,8 @@ __device__ __forceinline__ bool place(const Params& P, int& blk, int& j) {
   }
   return blk < P.n_blocks;
 }
+// A dimension of a grid holds fewer than 2^32 threads; a launch of more is accepted and runs in part.
+bool launches(int64_t grid, int threads) { return grid * threads < (int64_t)1 << 32; }
 int64_t grid_of(int64_t n_blocks, int Hkv) {
   if (Hkv <= 8 && 8 % Hkv == 0) return 8 * ((n_blocks + 8 / Hkv - 1) / (8 / Hkv));
   return n_blocks * Hkv;
@@ -1018,7 +1020,7 @@ int rl_packed_attn(const rl_packed_attn_desc* d, void* hip_stream) {
   Params P{};
   common(P, d);
   P.lse = d->lse;
-  if (grid_of(P.n_blocks, P.Hkv) > 0x7FFFFFFF) return -2;
+  if (!launches(grid_of(P.n_blocks, P.Hkv), THREADS)) return -2;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   const hipError_t e = d->d == 128 ? enqueue_forward<128>(P, st) : enqueue_forward<64>(P, st);
   return e == hipSuccess ? 0 : -5;
@@ -1036,7 +1038,7 @@ int rl_packed_attn_backward(const rl_packed_attn_backward_desc* d, void* hip_str
       !lies(d->dk, d->dk_stride, d->Hkv, d->d, d->T) || !lies(d->dv, d->dv_stride, d->Hkv, d->d, d->T)) return -2;
   Params P{};
   common(P, d);
-  if (grid_of(P.n_blocks, P.Hkv) >= 0x7FFFFFFF) return -2;
+  if (!launches(grid_of(P.n_blocks, P.Hkv) + 1, THREADS) || !launches(grid_of(key_blocks(P.T), P.Hkv), Dkdv<128>::THREADS)) return -2;
   const BackwardLayout l = layout_for(d);
   if (!d->workspace || d->workspace_bytes < l.total || ((uintptr_t)d->workspace & 255u)) return -3;
   P.dout = Tensor{static_cast<const char*>(d->dout), d->dout_stride * 2};

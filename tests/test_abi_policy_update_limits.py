@@ -1,0 +1,21 @@
+"""Sizes and factors at the ends of the ranges that the policy update's headers give: refused with the documented code, before anything is enqueued."""
+import pytest
+
+from paper_2512_21450_amd import binding as B
+from test_abi_policy_update import attn, attn_grad
+
+
+@pytest.mark.parametrize("kw", [dict(T=1 << 24, Hq=1 << 12, Hkv=1 << 12, d=64), dict(T=1 << 23, Hq=3 << 11, Hkv=1 << 11, d=128)])
+def test_packed_attn_grids_beyond_2_32_threads(kw):
+    """blocks of rows or keys times their threads: HIP runs a launch of 2^32 threads and more in part"""
+    q, k = dict(q_stride=kw["Hq"] * kw["d"]), dict(k_stride=kw["Hkv"] * kw["d"], v_stride=kw["Hkv"] * kw["d"])
+    assert B.rl_packed_attn_raw(attn(**kw, **q, **k, out_stride=q["q_stride"])) == -2
+    grads = dict(dout_stride=q["q_stride"], dq_stride=q["q_stride"], dk_stride=k["k_stride"], dv_stride=k["k_stride"])
+    assert B.rl_packed_attn_backward_raw(attn_grad(**kw, **q, **k, out_stride=q["q_stride"], **grads, workspace=0x1000, workspace_bytes=1 << 60)) == -2
+
+
+def test_packed_attn_backward_grid_of_key_blocks():
+    """64 heads of one key each: blocks of keys have more threads than blocks of rows"""
+    kw = dict(T=1 << 21, Hq=256, Hkv=256, d=64, q_stride=256 * 64, k_stride=256 * 64, v_stride=256 * 64, out_stride=256 * 64)
+    grads = dict(dout_stride=256 * 64, dq_stride=256 * 64, dk_stride=256 * 64, dv_stride=256 * 64, workspace=0x1000, workspace_bytes=1 << 60)
+    assert B.rl_packed_attn_backward_raw(attn_grad(**kw, **grads)) == -2
