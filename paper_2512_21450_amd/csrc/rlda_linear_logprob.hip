@@ -177,7 +177,7 @@ __global__ void __launch_bounds__(256) linear_logprob_merge_kernel(const Forward
     if (y >= P.s.V) lp = NAN;
     else if (y >= 0) {
       const float z = P.zy[n];
-      lp = z <= MASKED ? -INFINITY : (z - A.m - l2) * LN2;
+      lp = z <= MASKED && l2 == l2 ? -INFINITY : (z - A.m - l2) * LN2;                 // a logit of +inf leaves no distribution, for a masked token either
     }
     logprob[n] = lp;
   }

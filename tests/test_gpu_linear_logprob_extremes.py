@@ -38,6 +38,25 @@ def logit_bar(H, W, lse):
     return 8 * 2.0 ** -24 * np.sqrt(H.shape[1]) * (np.abs(H[ok]) @ np.abs(W).T).max() + 4 * 2.0 ** -24 * np.abs(lse[ok]).max()
 
 
+@pytest.mark.parametrize("N", [5, 300])
+def test_masked_token_of_a_row_without_a_distribution(B, N):
+    """next to a logit of +inf nothing has a log-prob, a masked token neither; without a live logit it is -inf"""
+    import torch
+    h, w, ids, _, _ = inputs(N, 64, 200, seed=N)
+    h[:, 0] = 1.0
+    w[:, 0] = 0.0
+    w[7, 0], w[9, 0] = float("inf"), float("-inf")
+    h[1::2, 0] = -1.0                                       # the two change places
+    h[2] = float("nan")
+    ids[0], ids[1], ids[2], ids[3] = 9, 7, 9, 5
+    got = B.rl_linear_logprob(h, w, ids)
+    with np.errstate(all="ignore"):
+        ref = dict(zip(("logprob", "lse", "entropy"), R.linear_logprob_ref(np64(h), np64(w), ids.cpu().numpy())))
+    assert np.isnan(ref["logprob"][[0, 1, 3]]).all() and np.isneginf(ref["logprob"][2])
+    for name, r in ref.items():
+        assert np.array_equal(np.isnan(np64(got[name])), np.isnan(r)) and np.array_equal(np.isneginf(np64(got[name])), np.isneginf(r)), name
+
+
 def test_more_workgroups_than_one_dimension_of_a_grid_holds(B):
     """2^22 tokens over 2^17 + 300 of 8 columns: more than 2^32 threads of tiles.  Rows from all over against 64 bits."""
     import torch
