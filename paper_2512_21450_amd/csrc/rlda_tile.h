@@ -38,6 +38,9 @@ __device__ __forceinline__ void landed_barrier() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(PENDING) : "memory");
 }
 
+// LDS writes of all wavefronts are there
+__device__ __forceinline__ void written_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
 enum Layout { K_COLS, K_ROWS };
 
 // one operand's tile of R (m or n) by BK; `ld2`: bytes between rows in memory
@@ -65,8 +68,8 @@ struct Operand {
       offset[i] = L == K_COLS ? (uint32_t)min(row, last) * ld2 + chunk * 16 : (uint32_t)row * ld2 + min(chunk, last / 8) * 16;
     }
   }
-  // the loads of k-step kt; only the first `chunks` 16-byte chunks of a row's BK (K_COLS) or `chunks` rows (K_ROWS) exist: the others
-  // read the last one, and the other operand holds zeros there
+  // the loads of k-step kt; only the first `exist` 16-byte chunks of a row's BK (K_COLS) or `exist` rows (K_ROWS) exist: the others
+  // read the last one, and clear() puts zeros over it once it has landed (zeros of the other operand would not do: 0 * infinity is not 0)
   template <bool FULL>
   __device__ __forceinline__ void issue(int kt, uint32_t lds, int wv, int lane, int exist) const {
     const char* const from = base + kt * step;
@@ -83,6 +86,14 @@ struct Operand {
         }
       }
       load_to_lds(from, o, lds + (wv * LOADS + i) * 1024);
+    }
+  }
+  __device__ __forceinline__ void clear(uint32_t lds, int wv, int lane, int exist) const {
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int row = (wv * LOADS + i) * ROWS_PER_LOAD + lane / CHUNKS;
+      if ((L == K_COLS ? (lane % CHUNKS) ^ pattern(row) : row) >= exist) *RLDA_AS3(u32x4, lds + (wv * LOADS + i) * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
     }
   }
 };
@@ -157,6 +168,10 @@ struct Tile {
       else                      landed_barrier();
       if (kt + STAGES - 1 < k1) issue(kt + STAGES - 1);
       const uint32_t cur = lds + ((kt - k0) & (STAGES - 1)) * STAGE;
+      if (kt == tail_step) {
+        a.clear(cur, wv, lane, tail);
+        written_barrier();
+      }
 #pragma unroll
       for (int ks = 0; ks < BK / 16; ++ks) {
         bf16x8 af[MT], bf[NT];

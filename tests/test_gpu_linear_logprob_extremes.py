@@ -38,6 +38,30 @@ def logit_bar(H, W, lse):
     return 8 * 2.0 ** -24 * np.sqrt(H.shape[1]) * (np.abs(H[ok]) @ np.abs(W).T).max() + 4 * 2.0 ** -24 * np.abs(lse[ok]).max()
 
 
+# a tile of each form; columns that end inside a step of 64, and on its end
+@pytest.mark.parametrize("N", [5, 60, 256, 300])
+@pytest.mark.parametrize("H", [8, 64, 72, 200])
+def test_infinite_weights_in_the_last_columns(B, N, H):
+    """A logit of +inf leaves a row without a distribution (NaN), one of -inf or NaN masks its token, wherever among the columns the infinity lies"""
+    h, w, ids, _, _ = inputs(N, H, 300, seed=N + H)
+    w[17, H - 1] = float("inf")
+    w[299, H - 1] = float("-inf")
+    h[:, H - 1] = 0.0                                       # both tokens masked
+    h[0::3, H - 1] = 1.0                                    # +inf, masked
+    ids[1], ids[3] = 17, 17
+    got = B.rl_linear_logprob(h, w, ids)
+    H64, W64 = np64(h), np64(w)
+    with np.errstate(all="ignore"):
+        ref = dict(zip(("logprob", "lse", "entropy"), R.linear_logprob_ref(H64, W64, ids.cpu().numpy())))
+    assert np.isnan(ref["lse"][0::3]).all() and np.isfinite(ref["lse"][1::3]).all()
+    bar = logit_bar(H64, W64, ref["lse"])
+    for name, r in ref.items():
+        g = np64(got[name])
+        assert np.array_equal(np.isnan(g), np.isnan(r)) and np.array_equal(np.isneginf(g), np.isneginf(r)), name
+        f = np.isfinite(r)
+        assert (np.abs(g[f] - r[f]) <= 2 * bar + 1e-6).all(), name
+
+
 @pytest.mark.parametrize("N", [5, 300])
 def test_masked_token_of_a_row_without_a_distribution(B, N):
     """next to a logit of +inf nothing has a log-prob, a masked token neither; without a live logit it is -inf"""
