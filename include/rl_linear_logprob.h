@@ -16,7 +16,8 @@
  *   dhidden  = dz . weight,    dweight = dz^T . hidden
  *
  * Ids, masked logits and rows without a live logit are as in rl_token_logprob.h (a negative id: logprob 0; id >= vocab: NaN; a
- * logit of -inf or NaN is masked).  Backward, an id outside [0, vocab) has no gradient of its logprob; a row without any
+ * logit of -inf or NaN is masked).  Backward, a masked logit has dz 0 and no part in dhidden, whatever its weights hold (it has both only where
+ * its token was sampled); an id outside [0, vocab) has no gradient of its logprob; a row without any
  * gradient (both 0, or no live logit) adds nothing to dweight, whatever its hidden state holds, and gets dhidden 0.
  *
  * bf16 data on the matrix cores with fp32 sums; logits, statistics and p are fp32, dz is rounded to bf16 before its two

@@ -121,7 +121,8 @@ def linear_logprob_ref(hidden, weight, token_ids, inv_temperature=1.0):
 
 
 def linear_logprob_grad_ref(hidden, weight, token_ids, g_logprob, g_entropy=None, inv_temperature=1.0):
-    """dhidden, dweight and the sums of |terms| of each.  A row with no gradient of its own adds nothing, whatever it holds."""
+    """dhidden, dweight and the sums of |terms| of each.  A row with no gradient of its own adds nothing, whatever it holds; dhidden sums
+    over the columns whose dz is not 0, so that a masked token's weights do not reach it."""
     h, w = np.asarray(hidden, np.float64), np.asarray(weight, np.float64)
     N, V = h.shape[0], w.shape[0]
     dz = np.zeros((N, V))
@@ -145,8 +146,11 @@ def linear_logprob_grad_ref(hidden, weight, token_ids, g_logprob, g_entropy=None
             dz[n, y] += gl
         dz[n] *= inv_temperature
     used = np.abs(dz).max(1) > 0
-    dh = np.zeros_like(h)
-    dh[used], hu = dz[used] @ w, h[used]
-    mh = np.zeros_like(h)
-    mh[used] = np.abs(dz[used]) @ np.abs(w)
+    hu = h[used]
+    finite = np.where(np.isfinite(w), w, 0.0)
+    dh, mh = dz @ finite, np.abs(dz) @ np.abs(finite)
+    for v in np.flatnonzero(~np.isfinite(w).all(1)):                          # of a masked token that was sampled
+        rest = np.where(np.isfinite(w[v]), 0.0, w[v])
+        for n in np.flatnonzero(dz[:, v]):
+            dh[n, rest != 0] += dz[n, v] * rest[rest != 0]
     return dh, dz[used].T @ hu, mh, np.abs(dz[used]).T @ np.abs(hu)

@@ -12,6 +12,10 @@
 //   dweight    m = hidden, n = vocabulary, k = tokens: both operands transposed
 // Scratch is zero where a token or a column does not exist, so that no product needs a mask.
 //
+// Weights that mask a token are infinite or NaN, and its dz, which is 0, would make NaN of them in dhidden.  A logit that is not finite says that there may
+// be some (hidden states that add anything are finite, unless they mask their row's every logit): the recomputation then raises a flag, and dhidden's
+// product reads the weights' infinities and NaN as zeros.  Only a masked token that was sampled has a dz; its infinities are added at the end.
+//
 // dz rounded to bf16 is off by the roundings of its few large elements; over many tokens they average out beside the result's own, over a
 // few they need not (2 tokens: dweight 2.4e-3 of its norm off against 1.6e-3).  Up to 32 tokens, whose tiles of 64 are half empty, the second half
 // holds what the first one's rounding left over: the products take it along as tokens of their own.
@@ -193,15 +197,18 @@ struct BackwardParams {
   int v0, v1;                                               // the piece
   float inv_t;
   bool twice;                                               // rows n + 32 of dz: what rounding left of rows n
+  int* odd;                                                 // raised where a logit is not finite
 };
 
 // rows of hidden states that add something, zeros for the others and up to whole k-steps in both directions
 __global__ void __launch_bounds__(256) linear_logprob_prepare_kernel(const char* hidden, int64_t hs, int N, int H, int V, int N64, int H64,
-    const int32_t* ids, const float* lse, const float* entropy, const float* gl, const float* ge, char* copy, float4* token, bool twice) {
+    const int32_t* ids, const float* lse, const float* entropy, const float* gl, const float* ge, char* copy, float4* token, bool twice,
+    int* odd) {
   const int row = (int)(blockIdx.y * GRID_X + blockIdx.x), n = twice ? row & 31 : row;                       // twice: rows n + 32 again
   if (row >= N64) return;
   bool live = n < N;
   if (token) {
+    if (row == 0 && threadIdx.x == 0) *odd = 0;
     float g = 0.f, e = 0.f, l = -INFINITY, ent = 0.f;
     if (live) {
       const int y = ids[n];
@@ -235,6 +242,14 @@ __global__ void __launch_bounds__(T::THREADS, T::THREADS == 512 ? 2 : 4) linear_
   const int vl = tm * T::BM + wm * T::MT * 32 + 4 * (lane >> 5);                       // in the piece, whose rows f.weight starts at
   const int V = P.v1 - P.v0;
   const int N64 = (P.f.s.N + 63) / 64 * 64;
+  float odd = 0.f;
+#pragma unroll
+  for (int j = 0; j < T::NT; ++j)
+#pragma unroll
+    for (int i = 0; i < T::MT; ++i)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) odd = fmaf(acc[i][j][x], 0.f, odd);
+  if (odd != 0.f) *P.odd = 1;
 #pragma unroll
   for (int j = 0; j < T::NT; ++j) {
     const int n = tn * T::BN + (wn * T::NT + j) * 32 + (lane & 31);
@@ -270,6 +285,7 @@ struct DhiddenParams {
   const __bf16* dz; int64_t ld;
   float* sum;                                               // [splits][N64][H]
   int first;                                                // the first piece: written, not added to
+  const int* odd;
 };
 
 template <typename T>
@@ -284,7 +300,7 @@ __global__ void __launch_bounds__(T::THREADS, T::THREADS == 512 ? 2 : 4) linear_
   const int nk = (P.V + T::BK - 1) / T::BK, tail = P.V % T::BK;
   const int k0 = (int)((int64_t)nk * split / P.splits), k1 = (int)((int64_t)nk * (split + 1) / P.splits);
   f32x16 acc[T::MT][T::NT];
-  T::run(a, b, k0, k1, tail ? nk - 1 : -1, tail, (uint32_t)(uintptr_t)RLDA_AS3(char, lds_all), acc);
+  T::template run<true>(a, b, k0, k1, tail ? nk - 1 : -1, tail, (uint32_t)(uintptr_t)RLDA_AS3(char, lds_all), acc, *P.odd != 0);
 #pragma unroll
   for (int j = 0; j < T::NT; ++j) {
     const int n = tn * T::BN + (wn * T::NT + j) * 32 + (lane & 31);
@@ -309,7 +325,8 @@ __global__ void __launch_bounds__(T::THREADS, T::THREADS == 512 ? 2 : 4) linear_
 // The splits' sums, rounded.  LANES threads share the slabs of four columns, in an order of their own that never changes: many slabs are those of few
 // tokens, whose sums would else be one long chain of loads (16 tokens, 2048 columns: 115 -> 7 us).
 template <int LANES>
-__global__ void __launch_bounds__(256) linear_logprob_round_kernel(const float* sum, int splits, int64_t slab, int N, int H, __bf16* out, int64_t stride, bool twice) {
+__global__ void __launch_bounds__(256) linear_logprob_round_kernel(const float* sum, int splits, int64_t slab, int N, int H, __bf16* out, int64_t stride, bool twice,
+    const int* odd, const __bf16* weight, int64_t ws, int V, const int32_t* ids, const float4* token, float inv_t) {
   __shared__ float4 part[256];
   constexpr int COLS = 256 / LANES;
   const int n = (int)(blockIdx.z * GRID_X + blockIdx.x);
@@ -337,7 +354,16 @@ __global__ void __launch_bounds__(256) linear_logprob_round_kernel(const float* 
       v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
     }
   }
-  if (h < H) *reinterpret_cast<bf16x4*>(out + (size_t)n * stride + h) = bf16x4{(__bf16)v.x, (__bf16)v.y, (__bf16)v.z, (__bf16)v.w};
+  if (h >= H) return;
+  const int y = ids[n];
+  if (*odd && y >= 0 && y < V && token[n].y != 0.f) {       // what dhidden's product left out: infinite weights of a masked token that was sampled
+    const bf16x4 w = *reinterpret_cast<const bf16x4*>(weight + (size_t)y * ws + h);
+    float* const to[4] = {&v.x, &v.y, &v.z, &v.w};
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      if (!(fabsf((float)w[x]) < INFINITY)) *to[x] += inv_t * token[n].y * (float)w[x];
+  }
+  *reinterpret_cast<bf16x4*>(out + (size_t)n * stride + h) = bf16x4{(__bf16)v.x, (__bf16)v.y, (__bf16)v.z, (__bf16)v.w};
 }
 
 struct DweightParams {
@@ -475,7 +501,7 @@ ForwardLayout forward_layout(int64_t N, int V, int H) {
 
 // Pieces of the vocabulary: dz of one is at most 256 MB, what the last-level cache holds.
 constexpr int64_t PIECE_BYTES = (int64_t)256 << 20;
-struct BackwardLayout { int64_t N64, H64; int piece, splits; size_t token, copy, dz, sum, total; };
+struct BackwardLayout { int64_t N64, H64; int piece, splits; size_t odd, token, copy, dz, sum, total; };
 BackwardLayout backward_layout(int64_t N, int V, int H, bool dhidden) {
   BackwardLayout l;
   l.N64 = up(N, 64); l.H64 = up(H, PAD);
@@ -494,8 +520,9 @@ BackwardLayout backward_layout(int64_t N, int V, int H, bool dhidden) {
     const float cost = (float)((tiles * s + held - 1) / held * held) / s * l.piece + 1000.f * s * tiles;
     if (cost < best) { best = cost; l.splits = s; }
   }
-  l.token = 0;
-  l.copy = align256((size_t)l.N64 * sizeof(float4));
+  l.odd = 0;
+  l.token = 256;
+  l.copy = l.token + align256((size_t)l.N64 * sizeof(float4));
   l.dz = l.copy + align256((size_t)l.N64 * l.H64 * 2);
   l.sum = l.dz + align256((size_t)l.N64 * l.piece * 2);
   l.total = l.sum + (dhidden ? align256((size_t)l.splits * l.N64 * H * sizeof(float)) : 0);
@@ -544,7 +571,7 @@ int rl_linear_logprob(const rl_linear_logprob_desc* d, void* hip_stream) {
   P.part = reinterpret_cast<float4*>(ws + l.part); P.zy = reinterpret_cast<float*>(ws + l.zy);
   if (H % PAD) {                                             // zeros behind the last column
     hipLaunchKernelGGL(linear_logprob_prepare_kernel, rows_grid(N), dim3(256), 0, st, static_cast<const char*>(P.hidden), P.hs, N, H, V, N, (int)l.H64,
-                       nullptr, nullptr, nullptr, nullptr, nullptr, ws + l.copy, nullptr, false);
+                       nullptr, nullptr, nullptr, nullptr, nullptr, ws + l.copy, nullptr, false, nullptr);
     P.hidden = ws + l.copy; P.hs = l.H64;
   }
   hipError_t e = f == SMALL32 ? enqueue_forward<Small32<K_COLS, K_COLS>>(P, st) : f == SMALL64 ? enqueue_forward<Small64<K_COLS, K_COLS>>(P, st)
@@ -581,8 +608,9 @@ int rl_linear_logprob_backward(const rl_linear_logprob_backward_desc* d, void* h
   const int N64 = (int)l.N64;
   const bool twice = N <= 32;
   float4* const token = reinterpret_cast<float4*>(ws + l.token);
+  int* const odd = reinterpret_cast<int*>(ws + l.odd);
   hipLaunchKernelGGL(linear_logprob_prepare_kernel, rows_grid(N64), dim3(256), 0, st, static_cast<const char*>(d->hidden_states), d->hidden_stride, N, H, V,
-                     N64, (int)l.H64, d->token_ids, d->lse, d->entropy, d->g_logprob, d->g_entropy, ws + l.copy, token, twice);
+                     N64, (int)l.H64, d->token_ids, d->lse, d->entropy, d->g_logprob, d->g_entropy, ws + l.copy, token, twice, odd);
   for (int v0 = 0; v0 < V; v0 += l.piece) {
     const int v1 = v0 + l.piece < V ? v0 + l.piece : V, cols = v1 - v0;
     const char* const w = static_cast<const char*>(d->weight) + (size_t)v0 * d->weight_stride * 2;
@@ -591,7 +619,7 @@ int rl_linear_logprob_backward(const rl_linear_logprob_backward_desc* d, void* h
     P.f.hidden = ws + l.copy; P.f.hs = l.H64; P.f.weight = w; P.f.ws = d->weight_stride; P.f.ids = d->token_ids;
     P.f.k2 = d->inv_temperature * LOG2E;
     P.token = token; P.dz = reinterpret_cast<__bf16*>(ws + l.dz); P.ld = l.piece;
-    P.v0 = v0; P.v1 = v1; P.inv_t = d->inv_temperature; P.twice = twice;
+    P.v0 = v0; P.v1 = v1; P.inv_t = d->inv_temperature; P.twice = twice; P.odd = odd;
     hipError_t e = f == SMALL64 ? enqueue_dz<Small64<K_COLS, K_COLS>>(P, st) : f == MID ? enqueue_dz<Mid<K_COLS, K_COLS>>(P, st)
                                                                                         : enqueue_dz<Big<K_COLS, K_COLS>>(P, st);
     if (e != hipSuccess) return -5;
@@ -599,7 +627,7 @@ int rl_linear_logprob_backward(const rl_linear_logprob_backward_desc* d, void* h
       DhiddenParams Q{};
       Q.tiles_m = (H + bm_of(f) - 1) / bm_of(f); Q.tiles_n = (N64 + bn_of(f) - 1) / bn_of(f); Q.splits = l.splits;
       Q.weight = w; Q.ws = d->weight_stride; Q.V = cols; Q.H = H; Q.N64 = N64; Q.dz = P.dz; Q.ld = P.ld;
-      Q.sum = reinterpret_cast<float*>(ws + l.sum); Q.first = v0 == 0;
+      Q.sum = reinterpret_cast<float*>(ws + l.sum); Q.first = v0 == 0; Q.odd = odd;
       e = f == SMALL64 ? enqueue_dhidden<Small64<K_ROWS, K_COLS>>(Q, st) : f == MID ? enqueue_dhidden<Mid<K_ROWS, K_COLS>>(Q, st)
                                                                                     : enqueue_dhidden<Big<K_ROWS, K_COLS>>(Q, st);
       if (e != hipSuccess) return -5;
@@ -621,12 +649,15 @@ int rl_linear_logprob_backward(const rl_linear_logprob_backward_desc* d, void* h
   if (d->dhidden) {
     const float* const sum = reinterpret_cast<const float*>(ws + l.sum);
     __bf16* const out = static_cast<__bf16*>(d->dhidden);
+    const __bf16* const w = static_cast<const __bf16*>(d->weight);
     const int64_t slab = (int64_t)N64 * H;
     const dim3 rows = rows_grid(N);
     if (l.splits >= 8)
-      hipLaunchKernelGGL(linear_logprob_round_kernel<16>, dim3(rows.x, (H + 63) / 64, rows.y), dim3(256), 0, st, sum, l.splits, slab, N, H, out, d->dhidden_stride, twice);
+      hipLaunchKernelGGL(linear_logprob_round_kernel<16>, dim3(rows.x, (H + 63) / 64, rows.y), dim3(256), 0, st, sum, l.splits, slab, N, H, out, d->dhidden_stride, twice,
+                         odd, w, d->weight_stride, V, d->token_ids, token, d->inv_temperature);
     else
-      hipLaunchKernelGGL(linear_logprob_round_kernel<1>, dim3(rows.x, (H + 1023) / 1024, rows.y), dim3(256), 0, st, sum, l.splits, slab, N, H, out, d->dhidden_stride, twice);
+      hipLaunchKernelGGL(linear_logprob_round_kernel<1>, dim3(rows.x, (H + 1023) / 1024, rows.y), dim3(256), 0, st, sum, l.splits, slab, N, H, out, d->dhidden_stride, twice,
+                         odd, w, d->weight_stride, V, d->token_ids, token, d->inv_temperature);
   }
   return hipGetLastError() == hipSuccess ? 0 : -5;
 }

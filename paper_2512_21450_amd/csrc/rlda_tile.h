@@ -88,12 +88,25 @@ struct Operand {
       load_to_lds(from, o, lds + (wv * LOADS + i) * 1024);
     }
   }
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
   __device__ __forceinline__ void clear(uint32_t lds, int wv, int lane, int exist) const {
-    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
       const int row = (wv * LOADS + i) * ROWS_PER_LOAD + lane / CHUNKS;
       if ((L == K_COLS ? (lane % CHUNKS) ^ pattern(row) : row) >= exist) *RLDA_AS3(u32x4, lds + (wv * LOADS + i) * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
+    }
+  }
+  // zeros in place of infinities and NaN
+  __device__ __forceinline__ void tidy(uint32_t lds, int wv, int lane) const {
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      u32x4 v = *RLDA_AS3(const u32x4, lds + (wv * LOADS + i) * 1024 + lane * 16);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const uint32_t lo = (v[x] & 0x7F80u) == 0x7F80u ? 0u : 0xFFFFu, hi = (v[x] & 0x7F800000u) == 0x7F800000u ? 0u : 0xFFFF0000u;
+        v[x] &= lo | hi;
+      }
+      *RLDA_AS3(u32x4, lds + (wv * LOADS + i) * 1024 + lane * 16) = v;
     }
   }
 };
@@ -139,9 +152,11 @@ struct Tile {
   typedef Operand<LB, BN, WAVES, BK> OB;
   static constexpr int STAGE = OA::BYTES + OB::BYTES, LDS = STAGES * STAGE;
 
-  // k-steps [k0, k1); `tail`: 16-byte chunks (K_COLS) or rows (K_ROWS) that A has in step tail_step
+  // k-steps [k0, k1); `tail`: 16-byte chunks (K_COLS) or rows (K_ROWS) that A has in step tail_step.  MAY_TIDY and `tidy`: A's infinities and NaN
+  // count as zeros.
+  template <bool MAY_TIDY = false>
   __device__ static __forceinline__ void run(const OA& a, const OB& b, int k0, int k1, int tail_step, int tail, uint32_t lds,
-                                             f32x16 (&acc)[MT][NT]) {
+                                             f32x16 (&acc)[MT][NT], bool tidy = false) {
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wv % WM, wn = wv / WM;
     Fragments<OA, LA, MT, BK> fa;
     Fragments<OB, LB, NT, BK> fb;
@@ -171,6 +186,12 @@ struct Tile {
       if (kt == tail_step) {
         a.clear(cur, wv, lane, tail);
         written_barrier();
+      }
+      if constexpr (MAY_TIDY) {
+        if (tidy) {
+          a.tidy(cur, wv, lane);
+          written_barrier();
+        }
       }
 #pragma unroll
       for (int ks = 0; ks < BK / 16; ++ks) {

@@ -81,6 +81,64 @@ def test_masked_token_of_a_row_without_a_distribution(B, N):
         assert np.array_equal(np.isnan(np64(got[name])), np.isnan(r)) and np.array_equal(np.isneginf(np64(got[name])), np.isneginf(r)), name
 
 
+@pytest.mark.parametrize("N,H,V", [(5, 64, 300), (40, 72, 129), (200, 136, 513), (256, 64, 300), (300, 264, 1000), (600, 64, 200)])
+def test_masked_tokens_weights_reach_no_hidden_states_gradient(B, N, H, V):
+    """Weights of -inf and NaN mask tokens.  dz is 0 there, and the sum over the vocabulary leaves them out: gradients are those of the weights with
+    zeros in these places; a row without a gradient, or without a live logit, gets zeros.  A masked token that was sampled has a gradient, and passes on
+    the infinity."""
+    import torch
+    h, w, ids, gl, ge = inputs(N, H, V, seed=N + H + V)
+    h[:, H - 1] = 1.0
+    w[:, H - 1] = 0.0
+    w[10:90, H - 1] = float("-inf")                         # masks these tokens
+    w[95] = float("nan")
+    w[V - 1, H - 1] = float("-inf")                         # the last row, which the last tile reads again past the end
+    ids[:] = torch.where((ids >= 10) & (ids < 100) | (ids == V - 1), 3, ids)
+    ids[1], gl[1] = 20, 1.5                                 # a masked token was sampled
+    gl[0] = ge[0] = 0
+    ids[2], ge[2] = -1, 0
+    h[3] = float("nan")                                     # no live logit
+    got = B.rl_linear_logprob(h, w, ids)
+    dh, dw = B.rl_linear_logprob_backward(h, w, ids, got["lse"], gl, entropy=got["entropy"], g_entropy=ge)
+    H64, W64, y = np64(h), np64(w), ids.cpu().numpy()
+    with np.errstate(all="ignore"):
+        lse = R.linear_logprob_ref(H64, W64, y)[1]
+        rh, rw, mh, mw = R.linear_logprob_grad_ref(H64, W64, y, np64(gl), np64(ge))
+    assert np.isneginf(rh[1, H - 1]) and np.isfinite(np.delete(rh.ravel(), H + H - 1)).all() and np.isfinite(rw).all()
+    assert (dh[0] == 0).all() and (dh[2] == 0).all() and (dh[3] == 0).all()
+    assert np.isneginf(np64(dh)[1, H - 1])
+    bar = logit_bar(H64, W64, lse)
+    for name, g, ref, mag in (("dhidden", np64(dh), rh, mh), ("dweight", np64(dw), rw, mw)):
+        f = np.isfinite(ref)
+        assert np.isfinite(g[f]).all(), name
+        assert (np.abs(g[f] - ref[f]) <= 1.1 * 2.0 ** -8 * (mag[f] + np.abs(ref[f])) + 2 * bar * mag[f] + 1e-30).all(), name
+
+
+def test_masked_tokens_in_several_pieces(B):
+    """20 thousand tokens: some 6.5 thousand columns of dz to a piece; masked tokens in the first and in the last one alone give zeros' gradients to the bit"""
+    import torch
+    N, H, V = 20000, 8, 15001
+    h, w, ids, gl, ge = inputs(N, H, V, seed=3)
+    ids[:] = ids.clamp(20, V - 20)
+    for at in (slice(0, 9), slice(V - 9, V)):
+        x, z = w.clone(), w.clone()
+        x[at, :4] = float("nan")
+        got = B.rl_linear_logprob(h, x, ids)
+        dh, dw = B.rl_linear_logprob_backward(h, x, ids, got["lse"], gl, entropy=got["entropy"], g_entropy=ge)
+        assert torch.isfinite(dh.float()).all() and torch.isfinite(dw.float()).all()
+        p = h.float() @ w.float().T
+        p[:, at] = -torch.inf
+        lp = torch.log_softmax(p, -1)
+        p = lp.exp()
+        lp = lp.masked_fill(p == 0, 0.0)
+        ent = -(p * lp).sum(-1)
+        dz = -p * (gl[:, None] + ge[:, None] * (lp + ent[:, None]))
+        dz.scatter_add_(1, ids.long()[:, None], gl[:, None])
+        z[at] = 0
+        for g, ref, mag in ((dh, dz @ z.float(), dz.abs() @ z.float().abs()), (dw, dz.T @ h.float(), dz.abs().T @ h.float().abs())):
+            assert ((g.float() - ref).abs() <= 1.1 * 2.0 ** -8 * (mag + ref.abs()) + 1e-4 * mag).all()
+
+
 def test_more_workgroups_than_one_dimension_of_a_grid_holds(B):
     """2^22 tokens over 2^17 + 300 of 8 columns: more than 2^32 threads of tiles.  Rows from all over against 64 bits."""
     import torch
