@@ -759,7 +759,7 @@ __global__ void __launch_bounds__(Dkdv<D>::THREADS, 2) packed_attn_dkdv_kernel(c
 #pragma unroll
   for (int db = 0; db < L::DB; ++db) { dk[db] = zeros(); dv[db] = zeros(); }
   const int rounds = (tiles + every - 1) / every;
-  const bool fine = rounds == 1 || __all(rhi - rlo <= FEW_ROWS);
+  const bool few = rounds == 1 || rhi - rlo <= FEW_ROWS, fine = __any(few && rhi > rlo);
   auto tile = [&](auto buffer, auto rest) {                 // rest: what the rounding of P and dS left over
     constexpr int Q = decltype(buffer)::value * M::STAGE, G = Q + M::TILEB, STATS = G + M::TILEB;
     constexpr bool REST = decltype(rest)::value;
@@ -768,6 +768,9 @@ __global__ void __launch_bounds__(Dkdv<D>::THREADS, 2) packed_attn_dkdv_kernel(c
       if (t >= every) issue(t - every, 1 - decltype(buffer)::value);
     }
     if (t < 0 || (t + 1) * M::STEP <= first_row || w0 >= nk) return;                       // none, or all before this wavefront's first key
+    if constexpr (REST) {
+      if (!__any(few && rlo < (t + 1) * M::STEP && rhi > t * M::STEP)) return;              // no row of such a key
+    }
     const RowFragments<D> rows = opaque(lane_rows), vrows = opaque(lane_vrows);
     const ColFragments<D> cols = opaque(lane_cols);
     typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -803,7 +806,10 @@ __global__ void __launch_bounds__(Dkdv<D>::THREADS, 2) packed_attn_dkdv_kernel(c
     }
     if constexpr (REST) {
 #pragma unroll
-      for (int x = 0; x < 16; ++x) { s[x] -= (float)(__bf16)s[x]; g[x] -= (float)(__bf16)g[x]; }
+      for (int x = 0; x < 16; ++x) {
+        s[x] = few ? s[x] - (float)(__bf16)s[x] : 0.f;
+        g[x] = few ? g[x] - (float)(__bf16)g[x] : 0.f;
+      }
     }
     bf16x8 p[2] = {pack(s, 0), pack(s, 1)}, d[2] = {pack(g, 0), pack(g, 1)};
     __builtin_amdgcn_s_setprio(1);
