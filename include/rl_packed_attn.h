@@ -42,7 +42,7 @@ typedef struct {
   int64_t  T;                /* tokens (>= 0)                                                     */
   int32_t  n_seqs;           /* sequences (>= 0)                                                  */
   int32_t  Hq, Hkv, d;       /* Hq % Hkv == 0, Hq / Hkv <= 64, d = 64 or 128                      */
-  float    scale;            /* any finite value                                                  */
+  float    scale;            /* |scale| <= 2e38                                                   */
   const void*    q;          /* [T, Hq, d]                                                        */
   const void*    k;          /* [T, Hkv, d]                                                       */
   const void*    v;          /* [T, Hkv, d]                                                       */
@@ -77,7 +77,7 @@ typedef struct {
 /*
  * Both: enqueue on `hip_stream` (hipStream_t as void*; NULL = default stream), asynchronous, allocate nothing.  Return 0
  * or a negative code with the meaning of the RLDA_ERR_* values of rl_decode_attn.h: -1 invalid argument (NULL where a tensor
- * is required, negative sizes, scale not finite), -2 unsupported (dtype, d, head counts, strides or alignment, T > 2^24,
+ * is required, negative sizes, |scale| > 2e38 or NaN), -2 unsupported (dtype, d, head counts, strides or alignment, T > 2^24,
  * heads times tokens beyond a launch's 2^32 threads: T * Hq or T * Hkv from 2^29 on),
  * -3 workspace, -4 struct_size, -5 HIP error.  With T = 0 nothing is read or written.
  */

@@ -59,10 +59,11 @@ struct Params {
   int QB, n_blocks;                                         // tokens a block of rows holds; blocks (of rows or keys)
   float scale, c;                                           // c = |scale| log2 e
   uint32_t flip, keep;                                      // queries get the scale's sign (xor) or are zeros (and)
+  float ck, k_down;                                         // c for dk and dv, whose keys are taken times k_down: c, and 1, but for scales next to 0
   float* lse;                                               // [Hq][T]
   int32_t* order;                                           // backward: [k_blocks] blocks of keys in the order in which they are begun, and as many of scratch
   int k_blocks;
-  float* stats;                                             // backward: [2][T][Hq]: -lse / |scale|, -D: what the sums of S and dP start from
+  float* stats;                                             // backward: [2][T][Hq]: -lse in units of ck, -D: what the sums of S and dP start from
   int splits;                                               // workgroups that share a block of keys
   float* part;                                              // their sums, if more than one: [splits][2][T][Hkv][d], dk and dv
 };
@@ -591,7 +592,7 @@ __global__ void __launch_bounds__(THREADS * TEAMS, 2) packed_attn_dq_kernel(cons
   }
   if (R.ok && lane < 32) {
     const int64_t i = (int64_t)R.token * P.Hq + R.head;
-    P.stats[i] = -lse2 / P.c;
+    P.stats[i] = -lse2 / P.ck;
     P.stats[(int64_t)P.T * P.Hq + i] = -(delta + sum);
   }
   if (!B.one || B.t0 - B.lo < FEW_KEYS) {                   // a row of the block has few keys
@@ -685,7 +686,7 @@ __device__ __forceinline__ void key_alone(const Params& P, int n, int j, int to_
       q.load(at(P.q, i, hh, L::ROWB), lane);
       d.load(at(P.dout, i, hh, L::ROWB), lane);
       const int64_t at_row = (int64_t)i * P.Hq + hh;
-      const float p = __builtin_amdgcn_exp2f(fmaf(q.dot(k), P.scale * LOG2E, P.stats[at_row] * P.c));
+      const float p = __builtin_amdgcn_exp2f(fmaf(q.dot(k), P.scale * LOG2E, P.stats[at_row] * P.ck));
       const float g = p * (d.dot(v) + P.stats[(int64_t)P.T * P.Hq + at_row]);
       av.add(p, d);
       ak.add(g, q);
@@ -752,6 +753,12 @@ __global__ void __launch_bounds__(Dkdv<D>::THREADS, 2) packed_attn_dkdv_kernel(c
   bf16x8 kf[L::KS], vf[M::V_IN_LDS ? 1 : L::KS];
   load_row<D>(at(P.k, ok ? key : 0, j, L::ROWB), lane, ok, P.flip, P.keep, kf);
   if constexpr (!M::V_IN_LDS) load_row<D>(at(P.v, ok ? key : 0, j, L::ROWB), lane, ok, 0u, ~0u, vf);
+  if (P.k_down != 1.f) {
+#pragma unroll
+    for (int ks = 0; ks < L::KS; ++ks)
+#pragma unroll
+      for (int x = 0; x < 8; ++x) kf[ks][x] = (__bf16)((float)kf[ks][x] * P.k_down);
+  }
   const int first_row = w0 * P.r, all_past = (w0 + 31) * P.r;
   const RowFragments<D> lane_rows(lds, lane), lane_vrows(lds_v + wv * 32 * L::ROWB, lane);
   const ColFragments<D> lane_cols(lds, lane);
@@ -795,7 +802,7 @@ __global__ void __launch_bounds__(Dkdv<D>::THREADS, 2) packed_attn_dkdv_kernel(c
     __builtin_amdgcn_s_setprio(0);
 #pragma unroll
     for (int x = 0; x < 16; ++x) {
-      s[x] = __builtin_amdgcn_exp2f(s[x] * P.c);
+      s[x] = __builtin_amdgcn_exp2f(s[x] * P.ck);
       g[x] *= s[x];
     }
     if (!whole || t * M::STEP < all_past || (t + 1) * M::STEP > n_rows) {
@@ -933,9 +940,14 @@ template <auto KERNEL> hipError_t enqueue(int lds, int64_t grid, hipStream_t st,
   return hipGetLastError();
 }
 
+constexpr float MOST_SCALE = 2e38f;                         // times log2 e it is still a number
+// Sums of S start from -lse / c in dk, dv.  Scales below this would take that past the largest number; keys are then taken times 2^-64 and c times 2^64.
+// Whatever that loses of a key (below 2^-62) is times a query (below 2^128) and c still far below a weight's own rounding.
+constexpr float LEAST_C = 0x1p-100f;
+
 int check(int dtype, int64_t T, int S, int Hq, int Hkv, int d, float scale) {
   if (T < 0 || S < 0 || Hq <= 0 || Hkv <= 0 || d <= 0) return -1;
-  if (!(scale >= -3.0e38f && scale <= 3.0e38f)) return -1;
+  if (!(scale >= -MOST_SCALE && scale <= MOST_SCALE)) return -1;
   if (dtype != 1 || (d != 64 && d != 128) || Hq % Hkv || Hq / Hkv > 64 || Hq > (1 << 16)) return -2;
   if (T > (1 << 24) || S > (1 << 30) || T * Hq > (int64_t)1 << 36) return -2;
   return 0;
@@ -957,6 +969,8 @@ template <typename Desc> void common(Params& P, const Desc* d) {
   P.scale = d->scale;
   const float m = d->scale < 0.f ? -d->scale : d->scale;
   P.c = m > 0.f ? m * LOG2E : 1.f;
+  const bool down = P.c < LEAST_C;
+  P.ck = down ? P.c * 0x1p64f : P.c; P.k_down = down ? 0x1p-64f : 1.f;
   P.flip = d->scale < 0.f ? 0x80008000u : 0u; P.keep = m > 0.f ? ~0u : 0u;
 }
 int check_backward(const rl_packed_attn_backward_desc* d) {

@@ -19,3 +19,9 @@ def test_packed_attn_backward_grid_of_key_blocks():
     kw = dict(T=1 << 21, Hq=256, Hkv=256, d=64, q_stride=256 * 64, k_stride=256 * 64, v_stride=256 * 64, out_stride=256 * 64)
     grads = dict(dout_stride=256 * 64, dq_stride=256 * 64, dk_stride=256 * 64, dv_stride=256 * 64, workspace=0x1000, workspace_bytes=1 << 60)
     assert B.rl_packed_attn_backward_raw(attn_grad(**kw, **grads)) == -2
+
+
+@pytest.mark.parametrize("scale", [2.5e38, -3e38])
+def test_scales_whose_base_2_form_is_no_number(scale):
+    assert B.rl_packed_attn_raw(attn(scale=scale)) == -1 and B.rl_packed_attn_backward_raw(attn_grad(scale=scale)) == -1
+    assert B.rl_packed_attn_backward_workspace_bytes(attn_grad(scale=scale)) == 0

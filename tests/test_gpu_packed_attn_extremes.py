@@ -89,3 +89,25 @@ def test_gradients_at_large_scores(B, Hq, Hkv, d, lens):
     lse = np.abs(np64(got[1])).max()
     assert M < 1000 and lse > 50
     check(got, *x, cu, scale, exponent=4 * 2.0 ** -24 * (np.sqrt(d) * (M + lse) + lse))
+
+
+@pytest.mark.parametrize("scale", [1e-29, 7e-31, -1e-33, 1e-36, 1e-38, -1e-38, 1e-42])
+def test_scales_next_to_nothing(B, scale):
+    """scores vanish: weights are equal, dv is their mean of dout; dq and dk vanish too"""
+    cu = [0, 100, 101, 230]
+    x = inputs(230, 4, 2, 64, seed=1)
+    scale = float(np.float32(scale))
+    check(run(B, *x, cu, scale), *x, cu, scale)
+
+
+@pytest.mark.parametrize("power", [-122, -110, -102, -98, 60, 90])
+def test_scales_that_make_up_for_the_inputs(B, power):
+    """q and k of 2^-(power / 2): the same scores at any scale, and the same bits of out and lse"""
+    import torch
+    cu = [0, 100, 101, 230]
+    q, k, v, dout = inputs(230, 4, 2, 64, seed=1)
+    ref = run(B, q, k, v, dout, cu, 0.125)
+    q2, k2 = (t.double().mul(2.0 ** (-power // 2)).bfloat16() for t in (q, k))
+    got = run(B, q2, k2, v, dout, cu, 0.125 * 2.0 ** power)
+    assert torch.equal(got[0], ref[0]) and torch.equal(got[1], ref[1])
+    check((*got[:2], *((t.double() * 2.0 ** (-power // 2)) for t in got[2:4]), got[4]), q, k, v, dout, cu, 0.125)
