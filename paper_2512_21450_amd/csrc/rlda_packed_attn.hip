@@ -25,7 +25,7 @@
 // over its three products), dk and dv 505 (0.77 over four), at 1.7 GHz with the matrix cores busy 46 to 50 % of the cycles; 14/2 heads of 64, 48 sequences of 24 to 340: 19, 31, 38.
 //
 // A masked weight is 0, but 0 times infinity is not: whatever a key outside a row's range holds would reach the row through a
-// product.  It cannot do so unseen, sums are then not finite; such rows (or keys) are computed again one by one over their own range.
+// product.  It cannot do so unseen, sums are then not finite; such rows (or keys) are computed again, with zeros in place of what is no number.
 #include <hip/hip_runtime.h>
 #include <stddef.h>
 #include <stdint.h>
@@ -228,35 +228,6 @@ __device__ __forceinline__ bool finite(const f32x16 (&v)[N]) {
   return z == 0.f;
 }
 
-// ---- rows one by one: a lane holds D / 64 columns
-template <int D> struct Columns {
-  static constexpr int N = D / 64;
-  float x[N];
-  __device__ __forceinline__ void load(const char* row, int lane) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = (float)reinterpret_cast<const __bf16*>(row)[lane * N + i];
-  }
-  __device__ __forceinline__ void store(char* row, int lane, float f) const {
-#pragma unroll
-    for (int i = 0; i < N; ++i) reinterpret_cast<__bf16*>(row)[lane * N + i] = (__bf16)(x[i] * f);
-  }
-  __device__ __forceinline__ void clear() {
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = 0.f;
-  }
-  __device__ __forceinline__ void add(float f, const Columns& o) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = fmaf(f, o.x[i], x[i]);
-  }
-  __device__ __forceinline__ float dot(const Columns& o) const {
-    float s = 0.f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) s = fmaf(x[i], o.x[i], s);
-#pragma unroll
-    for (int w = 1; w < 64; w <<= 1) s += __shfl_xor(s, w, 64);
-    return s;
-  }
-};
 __device__ __forceinline__ const char* at(const Tensor& t, int token, int head, int rowb) { return t.p + token * t.stride + (int64_t)head * rowb; }
 __device__ __forceinline__ char* to(const Tensor& t, int token, int head, int rowb) { return const_cast<char*>(at(t, token, head, rowb)); }
 
@@ -318,6 +289,249 @@ __device__ __forceinline__ void load_row(const char* p, int lane, bool ok, uint3
     for (int x = 0; x < 4; ++x) v[x] = (v[x] ^ flip) & keep;
     f[ks] = __builtin_bit_cast(bf16x8, v);
   }
+}
+
+// ---- sums that are not finite: rows (or keys) of a wavefront once more, in tiles of 32 of its own LDS, infinities and NaN of the matrices that weights are
+// multiplied with read as zeros.  What of them lies in a row's own range is added at the end: how many of a kind, a product of 0 and 1, says whether there
+// is one.  Weights go in two parts of 8 bits.  6000 tokens of 7/1 heads of 128 columns, forward and gradient, one token's q, k and v NaN: 0.8 to 1.8 ms, one
+// query alone up to 3.6 (0.56 without; one row or key after another 20 to 142).
+constexpr int AGAIN = 32;
+enum Kind { NOT_A_NUMBER = 1, PLUS_INF = 2, MINUS_INF = 4 };
+struct Kinds {                                              // kinds that were met, and the first and last tile that had any (all lanes the same)
+  int all, first, last;
+  __device__ __forceinline__ Kinds() : all(0), first(INT32_MAX), last(INT32_MIN) {}
+  __device__ __forceinline__ void add(int kinds, int tile) {
+    const int k = (__any(kinds & 1) ? 1 : 0) | (__any(kinds & 2) ? 2 : 0) | (__any(kinds & 4) ? 4 : 0);
+    if (k) { all |= k; first = min(first, tile); last = max(last, tile); }
+  }
+};
+
+// this wavefront's loads have landed, its LDS operations are done
+__device__ __forceinline__ void settled() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
+// What was computed of these before is computed again: it would be kept in registers of the loops in front otherwise.
+__device__ __forceinline__ void forget(int& a, int& b, int& c) { asm volatile("" : "+v"(a), "+v"(b), "+v"(c)); }
+// a lane or its partner in the other half
+__device__ __forceinline__ bool either_half(bool x) {
+  const uint64_t m = __ballot(x);
+  return (m | m >> 32) >> (threadIdx.x & 31) & 1;
+}
+// 32 rows from `base` on, of which those past `last` read it again
+template <int D>
+__device__ __forceinline__ void fetch32(const char* base, int64_t stride, int last, uint32_t lds, int lane) {
+  typedef Lds<D> L;
+#pragma unroll 1
+  for (int i = 0; i < AGAIN / L::RPL; ++i) {
+    const int row = i * L::RPL + lane / L::CH, chunk = (lane % L::CH) ^ L::pattern(row);
+    load_to_lds(base, (uint32_t)min(row, last) * (uint32_t)stride + chunk * 16, (uint32_t)uni(lds + i * 1024));
+  }
+}
+// the kinds that a tile holds (this lane's part of it), which then has zeros there; ones in the places of kinds `mark` and zeros elsewhere if there is any
+template <int D>
+__device__ __forceinline__ int tidy32(uint32_t lds, int lane, int mark) {
+  int kinds = 0;
+#pragma unroll 4
+  for (int i = 0; i < AGAIN / Lds<D>::RPL; ++i) {
+    const uint32_t a = lds + i * 1024 + lane * 16;
+    u32x4 v = *RLDA_AS3(const u32x4, a);
+    uint32_t any = 0;                                       // an exponent of ones, of either half of a word
+#pragma unroll
+    for (int x = 0; x < 4; ++x) any |= (v[x] & 0x7F807F80u) + 0x00800080u;
+    if (!(any & 0x80008000u) && !mark) continue;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      uint32_t w = 0;
+#pragma unroll
+      for (int half = 0; half < 32; half += 16) {
+        const uint32_t u = v[x] >> half & 0xFFFFu;
+        const int kind = (u & 0x7F80u) != 0x7F80u ? 0 : u & 0x7Fu ? NOT_A_NUMBER : u & 0x8000u ? MINUS_INF : PLUS_INF;
+        kinds |= kind;
+        w |= (mark ? (kind & mark ? 0x3F80u : 0u) : kind ? 0u : u) << half;
+      }
+      v[x] = w;
+    }
+    *RLDA_AS3(u32x4, a) = v;
+  }
+  settled();
+  return kinds;
+}
+// acc += (columns of the tile) (weights), both halves of 16 rows
+template <int D>
+__device__ __forceinline__ void add32(f32x16 (&acc)[Lds<D>::DB], const ColFragments<D>& at, const f32x16& w) {
+  const ColFragments<D> cols = opaque(at);
+#pragma unroll
+  for (int y = 0; y < 2; ++y) {
+    const bf16x8 p = pack(w, y);
+#pragma unroll
+    for (int db = 0; db < Lds<D>::DB; ++db) acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cols.get(y * 16 * Lds<D>::ROWB, db), p, acc[db], 0, 0, 0);
+  }
+}
+__device__ __forceinline__ f32x16 rest_of(const f32x16& w) {
+  f32x16 r;
+#pragma unroll
+  for (int x = 0; x < 16; ++x) r[x] = w[x] - (float)(__bf16)w[x];
+  return r;
+}
+
+// What is no number among a result's own terms goes into its columns: count(C, kind) says how many there are of a kind, put(db, x, value) replaces register x
+// of columns db.  Both infinities make NaN.
+template <int D, typename Count, typename Put>
+__device__ __forceinline__ void put_kinds(int kinds, Count count, Put put) {
+  uint64_t minus = 0;
+#pragma unroll 1
+  for (int kind = MINUS_INF; kind; kind >>= 1) {
+    if (!(kinds & kind)) continue;
+    f32x16 C[Lds<D>::DB];
+#pragma unroll
+    for (int db = 0; db < Lds<D>::DB; ++db) C[db] = zeros();
+    count(C, kind);
+#pragma unroll
+    for (int db = 0; db < Lds<D>::DB; ++db)
+#pragma unroll
+      for (int x = 0; x < 16; ++x)
+        if (C[db][x] > 0.f) {
+          const uint64_t bit = (uint64_t)1 << (16 * db + x);
+          put(db, x, kind == MINUS_INF ? -INFINITY : kind == PLUS_INF && !(minus & bit) ? INFINITY : NAN);
+          if (kind == MINUS_INF) minus |= bit;
+        }
+  }
+}
+__device__ __forceinline__ int column_of(int db, int x, int lane) { return 32 * db + m_of(x) + 4 * (lane >> 5); }
+
+// Rows of the forward call; bad_sum: lse as well.  Scores are rounded before a row's largest is taken off, so that rows of scores far beyond 2^31 (whose rounding is more than
+// a weight's range) come out too.
+template <int D>
+__device__ __forceinline__ void rows_again(const Params& P, const Block& B, Row R, bool bad, bool bad_sum, uint32_t lds, int lane) {
+  typedef Lds<D> L;
+  forget(lane, R.token, R.head);
+  constexpr int V = AGAIN * L::ROWB;
+  const int h4 = 4 * (lane >> 5);
+  const RowFragments<D> lane_rows(lds, lane);
+  const ColFragments<D> cols(lds + V, lane);
+  auto fetch = [&](const Tensor& t, int n0, uint32_t to) { fetch32<D>(t.p + uni(n0) * t.stride + (int64_t)B.j * L::ROWB, t.stride, B.hi - 1 - n0, to, lane); };
+  auto own = [&](int n0, int x) { const int n = n0 + h4 + m_of(x); return n >= R.start && n <= R.token; };
+  auto scores = [&](int n0) {
+    f32x16 s = zeros();
+    bf16x8 qf[L::KS];                                       // read again for every tile, which leaves registers to the sums
+    load_row<D>(at(P.q, R.token, R.head, L::ROWB), lane, R.ok, P.flip, P.keep, qf);
+    const RowFragments<D> rows = opaque(lane_rows);
+#pragma unroll
+    for (int ks = 0; ks < L::KS; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rows.get(0, ks), qf[ks], s, 0, 0, 0);
+#pragma unroll
+    for (int x = 0; x < 16; ++x) s[x] = own(n0, x) ? s[x] * P.c : -INFINITY;
+    return s;
+  };
+  float m = -INFINITY;
+  bool none = false;                                        // a score is +inf or NaN: so is all of the row, as it stands
+  for (int n0 = B.lo; n0 <= B.last; n0 += AGAIN) {
+    settled();
+    fetch(P.k, n0, lds);
+    settled();
+    const f32x16 s = scores(n0);
+#pragma unroll
+    for (int x = 0; x < 16; ++x) {
+      m = fmaxf(m, s[x]);
+      none |= !(s[x] < INFINITY);
+    }
+  }
+  m = half_max(m);
+  bad &= !either_half(none);
+  if (!__any(bad)) return;
+  f32x16 O[L::DB];
+#pragma unroll
+  for (int db = 0; db < L::DB; ++db) O[db] = zeros();
+  float l = 0.f;
+  Kinds kinds;
+#pragma unroll 1
+  for (int n0 = B.lo; n0 <= B.last; n0 += AGAIN) {
+    settled();
+    fetch(P.k, n0, lds);
+    fetch(P.v, n0, lds + V);
+    settled();
+    f32x16 p = scores(n0);
+#pragma unroll
+    for (int x = 0; x < 16; ++x) {
+      p[x] = p[x] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(p[x] - m);
+      l += p[x];
+    }
+    kinds.add(tidy32<D>(lds + V, lane, 0), n0);
+    add32<D>(O, cols, p);
+    add32<D>(O, cols, rest_of(p));
+  }
+  l = half_sum(l);
+  const float inv = l > 0.f ? 1.f / l : 0.f;                // no live score at all: 0
+  char* const out = to(P.out, R.token, R.head, L::ROWB);
+#pragma unroll
+  for (int db = 0; db < L::DB; ++db) store_block(out, db, O[db], inv, lane, bad);
+  if (P.lse && bad && bad_sum && lane < 32) P.lse[(int64_t)R.head * P.T + R.token] = l > 0.f ? (m + __log2f(l)) * LN2 : -INFINITY;
+  put_kinds<D>(kinds.all, [&](f32x16 (&C)[L::DB], int kind) {
+#pragma unroll 1
+    for (int n0 = kinds.first; n0 <= kinds.last; n0 += AGAIN) {
+      settled();
+      fetch(P.v, n0, lds + V);
+      settled();
+      tidy32<D>(lds + V, lane, kind);
+      f32x16 w;
+#pragma unroll
+      for (int x = 0; x < 16; ++x) w[x] = own(n0, x) ? 1.f : 0.f;
+      add32<D>(C, cols, w);
+    }
+  }, [&](int db, int x, float value) { if (bad) reinterpret_cast<__bf16*>(out)[column_of(db, x, lane)] = (__bf16)value; });
+}
+
+// dq of rows: an infinite or NaN key in a row's own range, whose weight is 0 at best, is NaN
+template <int D>
+__device__ __forceinline__ void dq_again(const Params& P, const Block& B, Row R, float lse2, float d_exact, bool bad, uint32_t lds, int lane) {
+  typedef Lds<D> L;
+  forget(lane, R.token, R.head);
+  constexpr int V = AGAIN * L::ROWB;
+  const int h4 = 4 * (lane >> 5);
+  const RowFragments<D> lane_rows(lds, lane);
+  const ColFragments<D> cols(lds, lane);
+  auto fetch = [&](const Tensor& t, int n0, uint32_t to) { fetch32<D>(t.p + uni(n0) * t.stride + (int64_t)B.j * L::ROWB, t.stride, B.hi - 1 - n0, to, lane); };
+  auto own = [&](int n0, int x) { const int n = n0 + h4 + m_of(x); return n >= R.start && n <= R.token; };
+  f32x16 A[L::DB];
+#pragma unroll
+  for (int db = 0; db < L::DB; ++db) A[db] = zeros();
+  Kinds kinds;
+#pragma unroll 1
+  for (int n0 = B.lo; n0 <= B.last; n0 += AGAIN) {
+    settled();
+    fetch(P.k, n0, lds);
+    fetch(P.v, n0, lds + V);
+    settled();
+    f32x16 s = zeros(), g = zeros();
+    bf16x8 qf[L::KS], gf[L::KS];
+    load_row<D>(at(P.q, R.token, R.head, L::ROWB), lane, R.ok, P.flip, P.keep, qf);
+    load_row<D>(at(P.dout, R.token, R.head, L::ROWB), lane, R.ok, 0u, ~0u, gf);
+    const RowFragments<D> rows = opaque(lane_rows);
+#pragma unroll
+    for (int ks = 0; ks < L::KS; ++ks) {
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rows.get(0, ks), qf[ks], s, 0, 0, 0);
+      g = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rows.get(V, ks), gf[ks], g, 0, 0, 0);
+    }
+#pragma unroll
+    for (int x = 0; x < 16; ++x) g[x] = own(n0, x) ? __builtin_amdgcn_exp2f(fmaf(s[x], P.c, -lse2)) * (g[x] - d_exact) : 0.f;
+    settled();
+    kinds.add(tidy32<D>(lds, lane, 0), n0);
+    add32<D>(A, cols, g);
+    add32<D>(A, cols, rest_of(g));
+  }
+  char* const dq = to(P.dq, R.token, R.head, L::ROWB);
+#pragma unroll
+  for (int db = 0; db < L::DB; ++db) store_block(dq, db, A[db], P.scale, lane, bad);
+  put_kinds<D>(kinds.all ? NOT_A_NUMBER : 0, [&](f32x16 (&C)[L::DB], int) {
+#pragma unroll 1
+    for (int n0 = kinds.first; n0 <= kinds.last; n0 += AGAIN) {
+      settled();
+      fetch(P.k, n0, lds);
+      settled();
+      tidy32<D>(lds, lane, NOT_A_NUMBER | PLUS_INF | MINUS_INF);
+      f32x16 w;
+#pragma unroll
+      for (int x = 0; x < 16; ++x) w[x] = own(n0, x) ? 1.f : 0.f;
+      add32<D>(C, cols, w);
+    }
+  }, [&](int db, int x, float value) { if (bad) reinterpret_cast<__bf16*>(dq)[column_of(db, x, lane)] = (__bf16)value; });
 }
 
 // Where there are few blocks of rows, what a call waits for is one block's tiles after one another: TEAMS of four wavefronts then hold the same rows,
@@ -422,31 +636,9 @@ __global__ void __launch_bounds__(THREADS * TEAMS, 2) packed_attn_kernel(const P
 #pragma unroll
   for (int db = 0; db < L::DB; ++db) store_block(out, db, O[db], inv, lane, R.ok);
   if (lse && R.ok && lane < 32) *lse = l == 0.f ? -INFINITY : (mc + __log2f(l)) * LN2;
-  // rows that are not finite, over their own keys
-  uint64_t bad = __ballot(R.ok && !(finite(O) && l < INFINITY));
-  bad = (bad | bad >> 32) & 0xFFFFFFFFu;
-  while (bad) {
-    const int src = __builtin_ctzll(bad);
-    bad &= bad - 1;
-    const int token = __builtin_amdgcn_readlane(R.token, src), head = __builtin_amdgcn_readlane(R.head, src), start = __builtin_amdgcn_readlane(R.start, src);
-    Columns<D> q, o, x;
-    q.load(at(P.q, token, head, L::ROWB), lane);
-    o.clear();
-    float m = -INFINITY, sum = 0.f;
-    for (int n = start; n <= token; ++n) {
-      x.load(at(P.k, n, B.j, L::ROWB), lane);
-      const float z = q.dot(x) * P.scale * LOG2E, m2 = fmaxf(m, z);
-      const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m2), e = z == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(z - m2);
-      sum = sum * alpha + e;
-#pragma unroll
-      for (int i = 0; i < Columns<D>::N; ++i) o.x[i] *= alpha;
-      x.load(at(P.v, n, B.j, L::ROWB), lane);
-      o.add(e, x);
-      m = m2;
-    }
-    o.store(to(P.out, token, head, L::ROWB), lane, start <= token ? 1.f / sum : 0.f);
-    if (P.lse && lane == 0) P.lse[(int64_t)head * P.T + token] = start <= token ? (m + __log2f(sum)) * LN2 : -INFINITY;
-  }
+  const bool bad_sum = !(l < INFINITY), bad = either_half(R.ok && (bad_sum || !finite(O)));
+  landed_barrier();                                         // nobody reads the buffers any more
+  if (__any(bad)) rows_again<D>(P, B, R, bad, bad_sum, (uint32_t)(uintptr_t)RLDA_AS3(char, lds_all) + wv * L::TILEB, lane);
 }
 
 // Blocks of keys differ in how many rows see them, and with some four of them to a compute unit one that is begun last shows: those of
@@ -634,24 +826,11 @@ __global__ void __launch_bounds__(THREADS * TEAMS, 2) packed_attn_dq_kernel(cons
   char* const dq = to(P.dq, R.token, R.head, L::ROWB);
 #pragma unroll
   for (int db = 0; db < L::DB; ++db) store_block(dq, db, A[db], P.scale, lane, R.ok);
-  uint64_t bad = __ballot(R.ok && !finite(A));
-  bad = (bad | bad >> 32) & 0xFFFFFFFFu;
-  while (bad) {
-    const int src = __builtin_ctzll(bad);
-    bad &= bad - 1;
-    const int token = __builtin_amdgcn_readlane(R.token, src), head = __builtin_amdgcn_readlane(R.head, src), start = __builtin_amdgcn_readlane(R.start, src);
-    const float ls = __shfl(lse2, src, 64), de = __shfl(delta + sum, src, 64);
-    Columns<D> q, d, k, v, a;
-    q.load(at(P.q, token, head, L::ROWB), lane);
-    d.load(at(P.dout, token, head, L::ROWB), lane);
-    a.clear();
-    for (int n = start; n <= token; ++n) {
-      k.load(at(P.k, n, B.j, L::ROWB), lane);
-      v.load(at(P.v, n, B.j, L::ROWB), lane);
-      a.add(__builtin_amdgcn_exp2f(fmaf(q.dot(k), P.scale * LOG2E, -ls)) * (d.dot(v) - de), k);
-    }
-    a.store(to(P.dq, token, head, L::ROWB), lane, P.scale);
-  }
+  const float d_exact = delta + sum;
+  // with lse or D NaN every key's part is NaN, as it stands; a token of no sequence gets 0
+  const bool bad = either_half(R.ok && !finite(A) && ((lse2 == lse2 && d_exact == d_exact) || R.start > R.token));
+  landed_barrier();                                         // nobody reads the buffers any more
+  if (__any(bad)) dq_again<D>(P, B, R, lse2, d_exact, bad, (uint32_t)(uintptr_t)RLDA_AS3(char, lds_all) + wv * L::TILEB, lane);
 }
 
 // 64 lanes x 4 bytes
@@ -672,27 +851,158 @@ template <int D> struct Dkdv {
   static constexpr int V_BYTES = V_IN_LDS ? KEYS * L::ROWB : 0, SUMS = 2 * L::DB * 16 * 256;            // of a wavefront
   static constexpr int RING = 2 * GROUPS * STAGE, BYTES = V_BYTES + (RING > 4 * SUMS ? RING : 4 * SUMS);
 };
-// dk and dv of one key, row by row
+// a key's sums: to its row of dk or dv, or to this workgroup's slab of sums where several share the block
 template <int D>
-__device__ __forceinline__ void key_alone(const Params& P, int n, int j, int to_token, int lane) {
+__device__ __forceinline__ float* part_of(const Params& P, int key, int j, bool values) {
+  const int64_t slab = (int64_t)P.T * P.Hkv * D;
+  return P.part + (2 * blockIdx.y + values) * slab + ((int64_t)key * P.Hkv + j) * D;
+}
+template <int D>
+__device__ __forceinline__ void store_key(const Params& P, int key, int j, const f32x16 (&sum)[Lds<D>::DB], bool values, bool these, int lane) {
   typedef Lds<D> L;
-  Columns<D> k, v, q, d, ak, av;
-  k.load(at(P.k, n, j, L::ROWB), lane);
-  v.load(at(P.v, n, j, L::ROWB), lane);
-  ak.clear();
-  av.clear();
-  for (int i = n; i < to_token; ++i)
-    for (int hh = j * P.r; hh < (j + 1) * P.r; ++hh) {
-      q.load(at(P.q, i, hh, L::ROWB), lane);
-      d.load(at(P.dout, i, hh, L::ROWB), lane);
-      const int64_t at_row = (int64_t)i * P.Hq + hh;
-      const float p = __builtin_amdgcn_exp2f(fmaf(q.dot(k), P.scale * LOG2E, P.stats[at_row] * P.ck));
-      const float g = p * (d.dot(v) + P.stats[(int64_t)P.T * P.Hq + at_row]);
-      av.add(p, d);
-      ak.add(g, q);
+  if (P.splits > 1) {
+    if (!these) return;
+    float* const p = part_of<D>(P, key, j, values) + 4 * (lane >> 5);
+#pragma unroll
+    for (int db = 0; db < L::DB; ++db)
+#pragma unroll
+      for (int x4 = 0; x4 < 4; ++x4)
+        *reinterpret_cast<float4*>(p + 32 * db + 8 * x4) = make_float4(sum[db][4 * x4], sum[db][4 * x4 + 1], sum[db][4 * x4 + 2], sum[db][4 * x4 + 3]);
+    return;
+  }
+  char* const p = to(values ? P.dv : P.dk, these ? key : 0, j, L::ROWB);
+#pragma unroll
+  for (int db = 0; db < L::DB; ++db) store_block(p, db, sum[db], values ? 1.f : P.scale, lane, these);
+}
+// fragments of the keys, one to a lane, as the scores of dk and dv take them
+template <int D>
+__device__ __forceinline__ void load_keys(const Params& P, int key, int j, bool ok, int lane, bf16x8 (&kf)[Lds<D>::KS]) {
+  load_row<D>(at(P.k, key, j, Lds<D>::ROWB), lane, ok, P.flip, P.keep, kf);
+  if (P.k_down != 1.f) {
+#pragma unroll
+    for (int ks = 0; ks < Lds<D>::KS; ++ks)
+#pragma unroll
+      for (int x = 0; x < 8; ++x) kf[ks][x] = (__bf16)((float)kf[ks][x] * P.k_down);
+  }
+}
+
+// dk and dv of a wavefront's keys, from the rows that this workgroup's wavefronts had
+template <int D>
+__device__ __forceinline__ void keys_again(const Params& P, int j, int key, int rlo, int rhi, int n0, int hi, bool bad_k, bool bad_v, uint32_t lds_v, int wv, int lane) {
+  typedef Lds<D> L;
+  typedef Dkdv<D> M;
+  forget(lane, key, rlo);
+  const bool ok = key < P.T;
+  const int h4 = 4 * (lane >> 5), n_rows = (hi - n0) * P.r, tiles = (n_rows + M::STEP - 1) / M::STEP;
+  const RowFragments<D> lane_vrows(lds_v + wv * 32 * L::ROWB, lane);
+  // The last rows whose lse or D is NaN: keys that the first sees have NaN in dk and dv, those that the other one sees in dk.  So it stands.
+  int no_lse = -1, no_d = -1;
+  for (int r0 = n_rows - 1; r0 >= 0 && no_lse < 0; r0 -= 4 * 64) {
+    float ls[4], de[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const int rr = max(r0 - 64 * x - lane, 0), tl = rr / P.r;
+      const int64_t i = (int64_t)(n0 + tl) * P.Hq + j * P.r + rr - tl * P.r;
+      ls[x] = P.stats[i];
+      de[x] = P.stats[(int64_t)P.T * P.Hq + i];
     }
-  ak.store(to(P.dk, n, j, L::ROWB), lane, P.scale);
-  av.store(to(P.dv, n, j, L::ROWB), lane, 1.f);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const uint64_t nl = __ballot(ls[x] != ls[x]), nd = __ballot(de[x] != de[x]);
+      if (nl && no_lse < 0) no_lse = max(r0 - 64 * x - __builtin_ctzll(nl), 0);
+      if (nd && no_d < 0) no_d = max(r0 - 64 * x - __builtin_ctzll(nd), 0);
+    }
+  }
+  bad_k &= !(no_lse >= rlo && no_lse < rhi) && !(no_d >= rlo && no_d < rhi);
+  bad_v &= !(no_lse >= rlo && no_lse < rhi);
+  if (!__any(bad_k || bad_v)) return;
+  // the rows that the wavefronts of this workgroup had, once more, as in the forward call: rows that do not see a key may hold anything
+  const uint32_t mine = lds_v + M::V_BYTES + wv * M::STAGE;
+  const RowFragments<D> mine_rows(mine, lane);
+  auto each = [&](int first_tile, int last_tile, bool bad, auto use) {
+#pragma unroll 1
+    for (int t = last_tile; t >= first_tile; --t) {
+      if ((tiles - 1 - t) / M::GROUPS % P.splits != (int)blockIdx.y || !__any(bad && rlo < (t + 1) * M::STEP && rhi > t * M::STEP)) continue;
+      const int first = (uint32_t)(uni(t) * M::STEP) / (uint32_t)P.r, rem = t * M::STEP - first * P.r, tt = n0 + first, last = hi - 1 - tt;
+      auto split = [&](int row, int& tl, int& hh) {
+        const uint32_t x = rem + row;
+        tl = x * P.magic >> 16;
+        hh = x - tl * P.r;
+        tl = min(tl, last);
+      };
+      settled();
+#pragma unroll 4
+      for (int i = 0; i < M::TILEB / 1024; ++i) {
+        const int row = i * L::RPL + lane / L::CH, chunk = (lane % L::CH) ^ L::pattern(row);
+        int tl, hh;
+        split(row, tl, hh);
+        const uint32_t in = hh * L::ROWB + chunk * 16;
+        load_to_lds(P.q.p + tt * P.q.stride + (int64_t)j * P.r * L::ROWB, tl * (uint32_t)P.q.stride + in, (uint32_t)uni(mine + i * 1024));
+        load_to_lds(P.dout.p + tt * P.dout.stride + (int64_t)j * P.r * L::ROWB, tl * (uint32_t)P.dout.stride + in, (uint32_t)uni(mine + M::TILEB + i * 1024));
+      }
+      int tl, hh;                                           // lse of the 32 rows, and D
+      split(lane & 31, tl, hh);
+      *RLDA_AS3(float, mine + 2 * M::TILEB + lane * 4) = P.stats[(lane >> 5) * (int64_t)P.T * P.Hq + (int64_t)(tt + tl) * P.Hq + j * P.r + hh];
+      settled();
+      use(t);
+    }
+  };
+  auto own = [&](int t, int x) { const int rr = t * M::STEP + h4 + m_of(x); return rr >= rlo && rr < rhi; };
+  f32x16 dk[L::DB], dv[L::DB];
+#pragma unroll
+  for (int db = 0; db < L::DB; ++db) { dk[db] = zeros(); dv[db] = zeros(); }
+  const ColFragments<D> qcols(mine, lane), gcols(mine + M::TILEB, lane);
+  Kinds q_kinds, g_kinds;
+  bf16x8 kf[L::KS], vf[M::V_IN_LDS ? 1 : L::KS];
+  load_keys<D>(P, ok ? key : 0, j, ok, lane, kf);
+  if constexpr (!M::V_IN_LDS) load_row<D>(at(P.v, ok ? key : 0, j, L::ROWB), lane, ok, 0u, ~0u, vf);
+  each(0, tiles - 1, bad_k || bad_v, [&](int t) {
+    f32x16 s = zeros(), g = zeros();
+    const RowFragments<D> rows = opaque(mine_rows), vrows = opaque(lane_vrows);
+#pragma unroll
+    for (int ks = 0; ks < L::KS; ++ks) {
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rows.get(0, ks), kf[ks], s, 0, 0, 0);
+      bf16x8 v;
+      if constexpr (M::V_IN_LDS) v = vrows.get(0, ks);
+      else                       v = vf[ks];
+      g = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rows.get(M::TILEB, ks), v, g, 0, 0, 0);
+    }
+#pragma unroll
+    for (int x = 0; x < 16; ++x) {
+      const uint32_t a = mine + 2 * M::TILEB + (h4 + m_of(x)) * 4;
+      s[x] = own(t, x) ? __builtin_amdgcn_exp2f((s[x] + *RLDA_AS3(const float, a)) * P.ck) : 0.f;
+      g[x] = own(t, x) ? s[x] * (g[x] + *RLDA_AS3(const float, a + 128)) : 0.f;
+    }
+    settled();
+    q_kinds.add(tidy32<D>(mine, lane, 0), t);
+    g_kinds.add(tidy32<D>(mine + M::TILEB, lane, 0), t);
+    add32<D>(dv, gcols, s);
+    add32<D>(dv, gcols, rest_of(s));
+    add32<D>(dk, qcols, g);
+    add32<D>(dk, qcols, rest_of(g));
+  });
+  store_key<D>(P, key, j, dk, false, bad_k, lane);
+  store_key<D>(P, key, j, dv, true, bad_v, lane);
+#pragma unroll 1
+  for (int values = 1; values >= 0; --values) {             // dv, then dk: an infinite or NaN query, whose weight is 0 at best, makes it NaN
+    const bool bad = values ? bad_v : bad_k;
+    const uint32_t tile = mine + (values ? M::TILEB : 0);
+    const ColFragments<D> cols(tile, lane);
+    put_kinds<D>(values ? g_kinds.all : q_kinds.all ? NOT_A_NUMBER : 0, [&](f32x16 (&C)[L::DB], int kind) {
+      each(values ? g_kinds.first : q_kinds.first, values ? g_kinds.last : q_kinds.last, bad, [&](int t) {
+        tidy32<D>(tile, lane, values ? kind : NOT_A_NUMBER | PLUS_INF | MINUS_INF);
+        f32x16 w;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) w[x] = own(t, x) ? 1.f : 0.f;
+        add32<D>(C, cols, w);
+      });
+    }, [&](int db, int x, float value) {
+      if (!bad) return;
+      const int col = column_of(db, x, lane);
+      if (P.splits > 1) part_of<D>(P, key, j, values)[col] = value;
+      else              reinterpret_cast<__bf16*>(to(values ? P.dv : P.dk, key, j, L::ROWB))[col] = (__bf16)value;
+    });
+  }
 }
 
 template <int D>
@@ -866,33 +1176,11 @@ __global__ void __launch_bounds__(Dkdv<D>::THREADS, 2) packed_attn_dkdv_kernel(c
     }
   }
   if (group > 0) return;
-  if (P.splits > 1) {
-    const int64_t slab = (int64_t)P.T * P.Hkv * D;
-    float* const p = P.part + 2 * blockIdx.y * slab + ((int64_t)key * P.Hkv + j) * D + h4;
-    if (!ok) return;
-#pragma unroll
-    for (int db = 0; db < L::DB; ++db)
-#pragma unroll
-      for (int x4 = 0; x4 < 4; ++x4) {
-        *reinterpret_cast<float4*>(p + 32 * db + 8 * x4) = make_float4(dk[db][4 * x4], dk[db][4 * x4 + 1], dk[db][4 * x4 + 2], dk[db][4 * x4 + 3]);
-        *reinterpret_cast<float4*>(p + slab + 32 * db + 8 * x4) = make_float4(dv[db][4 * x4], dv[db][4 * x4 + 1], dv[db][4 * x4 + 2], dv[db][4 * x4 + 3]);
-      }
-    return;
-  }
-  char* const pk = to(P.dk, ok ? key : 0, j, L::ROWB);
-  char* const pv = to(P.dv, ok ? key : 0, j, L::ROWB);
-#pragma unroll
-  for (int db = 0; db < L::DB; ++db) {
-    store_block(pk, db, dk[db], P.scale, lane, ok);
-    store_block(pv, db, dv[db], 1.f, lane, ok);
-  }
-  uint64_t bad = __ballot(ok && !(finite(dk) && finite(dv)));
-  bad = (bad | bad >> 32) & 0xFFFFFFFFu;
-  while (bad) {
-    const int src = __builtin_ctzll(bad);
-    bad &= bad - 1;
-    key_alone<D>(P, __builtin_amdgcn_readlane(key, src), j, n0 + __builtin_amdgcn_readlane(rhi, src) / P.r, lane);
-  }
+  store_key<D>(P, key, j, dk, false, ok, lane);
+  store_key<D>(P, key, j, dv, true, ok, lane);
+  const bool bad_k = either_half(ok && !finite(dk)), bad_v = either_half(ok && !finite(dv));
+  landed_barrier();                                         // the other wavefront has read its sums
+  if (__any(bad_k || bad_v)) keys_again<D>(P, j, key, rlo, rhi, n0, hi, bad_k, bad_v, lds_v, wv, lane);
 }
 
 // The sums of the workgroups that share a block of keys, in their order: a wavefront to a key and head.
@@ -903,25 +1191,17 @@ __global__ void __launch_bounds__(256) packed_attn_join_kernel(const Params P) {
   if (i >= P.T * P.Hkv) return;
   const int n = i / P.Hkv, j = i - n * P.Hkv;
   const int64_t slab = (int64_t)P.T * P.Hkv * D;
-  Columns<D> k, v;
-  k.clear();
-  v.clear();
+  constexpr int N = D / 64;
+  float k[N] = {}, v[N] = {};
   for (int s = 0; s < P.splits; ++s) {
-    const float* const p = P.part + 2 * s * slab + (int64_t)i * D + lane * Columns<D>::N;
+    const float* const p = P.part + 2 * s * slab + (int64_t)i * D + lane * N;
 #pragma unroll
-    for (int x = 0; x < Columns<D>::N; ++x) { k.x[x] += p[x]; v.x[x] += p[slab + x]; }
+    for (int x = 0; x < N; ++x) { k[x] += p[x]; v[x] += p[slab + x]; }
   }
-  float z = 0.f;
+  __bf16* const pk = reinterpret_cast<__bf16*>(to(P.dk, n, j, L::ROWB)) + lane * N;
+  __bf16* const pv = reinterpret_cast<__bf16*>(to(P.dv, n, j, L::ROWB)) + lane * N;
 #pragma unroll
-  for (int x = 0; x < Columns<D>::N; ++x) z = fmaf(k.x[x], 0.f, fmaf(v.x[x], 0.f, z));
-  if (__all(z == 0.f)) {
-    k.store(to(P.dk, n, j, L::ROWB), lane, P.scale);
-    v.store(to(P.dv, n, j, L::ROWB), lane, 1.f);
-    return;
-  }
-  int start, end;
-  if (!sequence_of_all(P, n, start, end)) end = n;
-  key_alone<D>(P, n, j, end, lane);
+  for (int x = 0; x < N; ++x) { pk[x] = (__bf16)(k[x] * P.scale); pv[x] = (__bf16)v[x]; }
 }
 
 // ---- host side

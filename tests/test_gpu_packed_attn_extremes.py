@@ -111,3 +111,94 @@ def test_scales_that_make_up_for_the_inputs(B, power):
     got = run(B, q2, k2, v, dout, cu, 0.125 * 2.0 ** power)
     assert torch.equal(got[0], ref[0]) and torch.equal(got[1], ref[1])
     check((*got[:2], *((t.double() * 2.0 ** (-power // 2)) for t in got[2:4]), got[4]), q, k, v, dout, cu, 0.125)
+
+
+@pytest.mark.parametrize("Hq,Hkv,d,extra", [(4, 2, 128, 0), (4, 2, 64, 0), (4, 2, 128, 9000)])
+def test_infinities_in_a_rows_own_range(B, Hq, Hkv, d, extra):
+    """An infinite value makes its column of all rows that see it infinite, both kinds or a NaN make it NaN; an infinite dout the same of dv.  Everything else is
+    what zeros in these places give.  (extra: so many tokens behind, which take a block of keys from several workgroups to one)"""
+    import torch
+    cu = [0, 40, 240] + ([240 + extra] if extra else [])
+    T, scale = cu[-1], 0.09
+    q, k, v, dout = inputs(T, Hq, Hkv, d, seed=d)
+    x = [t.clone() for t in (q, k, v, dout)]
+    inf, nan = float("inf"), float("nan")
+    x[2][70, :, 5], x[2][100, :, 5], x[2][130, :, 7], x[2][60, 0, d - 1], x[2][150] = inf, -inf, nan, -inf, 0
+    v[70, :, 5] = v[100, :, 5] = v[130, :, 7] = v[60, 0, d - 1] = v[150] = 0
+    c = torch.tensor(cu, dtype=torch.int32, device="cuda")
+    out, lse = B.rl_packed_attn(*x[:3], c, scale)
+    ref, rl, mag = R.packed_attn_ref(*(np64(t)[:240] for t in (q, k, v)), cu[:3], scale)
+    want = ref.copy()
+    want[70:100, :, 5], want[100:, :, 5], want[130:, :, 7], want[60:, :Hq // Hkv, d - 1] = inf, nan, nan, -inf
+    got, fin = np64(out)[:240], np.isfinite(want)
+    assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(got[~fin & ~np.isnan(want)], want[~fin & ~np.isnan(want)])
+    assert (np.abs(got - ref)[fin] <= (1.1 * U * (mag + np.abs(ref)) + 2e-5 * mag)[fin]).all()
+    assert (np.abs(np64(lse)[:, :240] - rl) <= 2e-5 + 2e-7 * np.abs(rl)).all()
+    # an infinite dout
+    out, lse = B.rl_packed_attn(q, k, v, c, scale)
+    dout[110, 0, 3] = dout[170, 1, 3] = dout[120, Hq - 1, 4] = 0
+    x[3][:] = dout
+    x[3][110, 0, 3], x[3][170, 1, 3], x[3][120, Hq - 1, 4] = inf, -inf, nan
+    dq, dk, dv = (np64(t)[:240] for t in B.rl_packed_attn_backward(x[3], q, k, v, out, lse, c, scale))
+    bar = 1.1 * U * (mag + np.abs(ref)) + 2e-5 * mag
+    rq, _, rv, mq, _, mv = R.packed_attn_grad_ref(np64(dout)[:240], *(np64(t)[:240] for t in (q, k, v)), cu[:3], scale, out_error=bar)
+    want = rv.copy()
+    want[40:111, 0, 3], want[111:171, 0, 3], want[40:121, Hkv - 1, 4] = nan, -inf, nan             # up to 110: both infinities, of two heads
+    fin = np.isfinite(want)
+    assert np.array_equal(np.isnan(dv), np.isnan(want)) and np.array_equal(dv[~fin & ~np.isnan(want)], want[~fin & ~np.isnan(want)])
+    assert (np.abs(dv - rv)[fin] <= (1.1 * U * (mv + np.abs(rv)) + 1e-4 * mv)[fin]).all()
+    odd = np.zeros((240, Hq), bool)
+    odd[110, 0] = odd[170, 1] = odd[120, Hq - 1] = True
+    assert not np.isfinite(dq[odd]).any() and (np.abs(dq - rq)[~odd] <= (1.1 * U * (mq + np.abs(rq)) + 1e-4 * mq)[~odd]).all()
+    seen = np.zeros((240, Hkv), bool)
+    seen[40:171, 0] = seen[40:121, Hkv - 1] = True
+    assert not np.isfinite(dk[seen]).any() and np.isfinite(dk[~seen]).all()
+
+
+def times(f, n=5):
+    import torch
+    best = float("inf")
+    for _ in range(n):
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        f()
+        b.record()
+        b.synchronize()
+        best = min(best, a.elapsed_time(b))
+    return best
+
+
+@pytest.mark.parametrize("where", ["q", "k", "v", "kv"])
+@pytest.mark.parametrize("token", [0, 2000, 5999])
+def test_not_a_number_in_a_long_sequence(B, where, token):
+    """NaN in one token of 6000: rows from it on are NaN (a query's own row alone), the others as ever; and a call takes the time of a few, not of a walk
+    over the keys for every row"""
+    import torch
+    T, Hq, Hkv, d, scale = 6000, 7, 1, 128, 0.09
+    cu = torch.tensor([0, T], dtype=torch.int32, device="cuda")
+    q, k, v, dout = inputs(T, Hq, Hkv, d, seed=2)
+    ref = run(B, q, k, v, dout, [0, T], scale)
+
+    def step():
+        out, lse = B.rl_packed_attn(q, k, v, cu, scale)
+        return (out, lse, *B.rl_packed_attn_backward(dout, q, k, v, out, lse, cu, scale))
+    usual = times(step)
+    for t, name in ((q, "q"), (k, "k"), (v, "v")):
+        if name in where:
+            t[token] = float("nan")
+    out, lse, dq, dk, dv = step()
+    rows = torch.zeros(T, dtype=torch.bool, device="cuda")
+    rows[token:token + 1 if where == "q" else T] = True
+    assert torch.isnan(out[rows].float()).all() and torch.isfinite(out[~rows].float()).all()
+    assert (torch.isnan(lse[:, rows]).all() if where != "v" else torch.equal(lse, ref[1])) and torch.equal(lse[:, ~rows], ref[1][:, ~rows])
+    assert ((out[~rows].float() - ref[0][~rows].float()).abs() <= 4 * U * ref[0][~rows].float().abs() + 2e-2).all()
+    assert torch.isnan(dq[rows].float()).all() and torch.isfinite(dq[~rows].float()).all()
+    assert ((dq[~rows].float() - ref[2][~rows].float()).abs() <= 4 * U * ref[2][~rows].float().abs() + 2e-2).all()
+    # every key up to the last NaN row is seen by one
+    last = token + 1 if where == "q" else T
+    assert torch.isnan(dk[:last].float()).all() and torch.isfinite(dk[last:].float()).all() and torch.isfinite(dv[last:].float()).all()
+    if where != "v":
+        assert torch.isnan(dv[:last].float()).all()
+    else:
+        assert torch.equal(dv, ref[4])
+    assert times(step) <= 10 * usual + 1.0
