@@ -636,7 +636,7 @@ __global__ void __launch_bounds__(THREADS * TEAMS, 2) packed_attn_kernel(const P
 #pragma unroll
   for (int db = 0; db < L::DB; ++db) store_block(out, db, O[db], inv, lane, R.ok);
   if (lse && R.ok && lane < 32) *lse = l == 0.f ? -INFINITY : (mc + __log2f(l)) * LN2;
-  const bool bad_sum = !(l < INFINITY), bad = either_half(R.ok && (bad_sum || !finite(O)));
+  const bool bad_sum = !(l < INFINITY) || (l == 0.f && R.start <= R.token), bad = either_half(R.ok && (bad_sum || !finite(O)));
   landed_barrier();                                         // nobody reads the buffers any more
   if (__any(bad)) rows_again<D>(P, B, R, bad, bad_sum, (uint32_t)(uintptr_t)RLDA_AS3(char, lds_all) + wv * L::TILEB, lane);
 }

@@ -202,3 +202,16 @@ def test_not_a_number_in_a_long_sequence(B, where, token):
     else:
         assert torch.equal(dv, ref[4])
     assert times(step) <= 10 * usual + 1.0
+
+
+@pytest.mark.parametrize("d,T", [(64, 5), (128, 150), (128, 900)])
+def test_scores_far_below_zero(B, d, T):
+    """every score of a row near -1e32: the largest of them still is the row's reference"""
+    import torch
+    cu = [0, 3, T]
+    q, k, v, dout = inputs(T, 4, 2, d, seed=d)
+    q[:], k[:] = 2.0 ** 53, -2.0 ** 53
+    out, lse = B.rl_packed_attn(q, k, v, torch.tensor(cu, dtype=torch.int32, device="cuda"), 0.125)
+    ref, rl, mag = R.packed_attn_ref(*(np64(t) for t in (q, k, v)), cu, 0.125)
+    assert (np.abs(np64(lse) - rl) <= 1e-6 * np.abs(rl)).all()
+    assert (np.abs(np64(out) - ref) <= 1.1 * U * (mag + np.abs(ref)) + 2e-5 * mag).all()
