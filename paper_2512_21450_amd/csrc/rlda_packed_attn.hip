@@ -61,7 +61,7 @@ struct Params {
   uint32_t flip, keep;                                      // queries get the scale's sign (xor) or are zeros (and)
   float ck, k_down;                                         // c for dk and dv, whose keys are taken times k_down: c, and 1, but for scales next to 0
   float* lse;                                               // [Hq][T]
-  int32_t* order;                                           // backward: [k_blocks] blocks of keys in the order in which they are begun, and as many of scratch
+  int32_t* order;                                           // backward: [k_blocks] blocks of keys in the order in which they are begun, and as many of scratch; or null
   int k_blocks;
   float* stats;                                             // backward: [2][T][Hq]: -lse in units of ck, -D: what the sums of S and dP start from
   int splits;                                               // workgroups that share a block of keys
@@ -642,10 +642,14 @@ __global__ void __launch_bounds__(THREADS * TEAMS, 2) packed_attn_kernel(const P
 }
 
 // Blocks of keys differ in how many rows see them, and with some four of them to a compute unit one that is begun last shows: those of
-// many rows come first, in ORDERS classes (not sorted, so that blocks of a sequence, which read the same rows, stay together).  By one wavefront
-// beside the dq blocks.  Ten trajectories of up to 1996 tokens of 28/4 heads, dq and dk, dv together: 945 us without, 928 with 2 classes, 935
-// with 4, 924 with 8, 940 with 16; 16 of 200 to 2000 tokens of 14/2 heads of 64 columns, dk, dv: 243 without, 184.
+// many rows come first, in ORDERS classes (not sorted, so that blocks of a sequence, which read the same rows, stay together; 2, 4 and 16 classes were
+// within 1 % of 8).  By one wavefront beside the dq blocks, whose time grows with the tokens; and where workgroups are many nothing is gained, and some of
+// the reads shared by the heads of a token are lost.  us of the gradient, as they lie / in order (blocks x KV heads): 14/2 heads of 64 columns, 200 to 2000
+// tokens a sequence, 22848 tokens 394 / 310, 90821 (1420 x 2) 1205 / 1114, 131079 (2049 x 2) 1678 / 1629, 24 to 340 tokens 22008 141 / 124, 131113 684 / 710;
+// 28/4 of 128, 1280 to 1996 tokens, 9351 523 / 448, 16469 (258 x 4) 832 / 821, 25829 (404 x 4) 1276 / 1303, 66530 3252 / 3371; 2/1 of 64, 100 tokens, 22000
+// 45 / 42, 131100 (2049 x 1) 158 / 205, 2^20 1290 / 1950.
 constexpr int KEY_BLOCK = 64, ORDERS = 8;
+bool ordered(int64_t k_blocks, int Hkv, int d) { return k_blocks <= 1536 && k_blocks * Hkv <= (d == 128 ? 1536 : 3072); }
 __device__ __forceinline__ void order_key_blocks(const Params& P) {
   const int lane = threadIdx.x & 63, n = P.k_blocks;
   if (threadIdx.x >= 64) return;
@@ -691,7 +695,7 @@ __global__ void __launch_bounds__(THREADS * TEAMS, 2) packed_attn_dq_kernel(cons
   extern __shared__ __attribute__((aligned(1024))) char lds_all[];
   const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6), wv = wave % WAVES, team = wave / WAVES, h4 = 4 * (lane >> 5);
   if (blockIdx.x == gridDim.x - 1) {                        // one workgroup more than there are blocks
-    order_key_blocks(P);
+    if (P.order) order_key_blocks(P);
     return;
   }
   Block B;
@@ -1013,7 +1017,7 @@ __global__ void __launch_bounds__(Dkdv<D>::THREADS, 2) packed_attn_dkdv_kernel(c
   const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6), wv = wave & 1, group = wave >> 1, h4 = 4 * (lane >> 5);
   int blk, j;
   if (!place(P, blk, j)) return;
-  blk = uni(P.order[blk]);
+  if (P.order) blk = uni(P.order[blk]);
   const int n0 = blk * M::KEYS, nk = min(M::KEYS, P.T - n0), w0 = 32 * wv;
   const uint32_t lds_v = (uint32_t)(uintptr_t)RLDA_AS3(char, lds_all), lds = lds_v + M::V_BYTES + group * 2 * M::STAGE;
   int start, end, hi = n0 + nk;                             // rows of tokens [n0, hi) may see a key of the block
@@ -1348,7 +1352,7 @@ int rl_packed_attn_backward(const rl_packed_attn_backward_desc* d, void* hip_str
   P.lse = const_cast<float*>(d->lse);
   char* const ws = static_cast<char*>(d->workspace);
   P.stats = reinterpret_cast<float*>(ws);
-  P.order = reinterpret_cast<int32_t*>(ws + l.order);
+  P.order = ordered(key_blocks(P.T), P.Hkv, d->d) ? reinterpret_cast<int32_t*>(ws + l.order) : nullptr;
   P.part = reinterpret_cast<float*>(ws + l.part);
   P.splits = l.splits;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);

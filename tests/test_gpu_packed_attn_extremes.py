@@ -215,3 +215,22 @@ def test_scores_far_below_zero(B, d, T):
     ref, rl, mag = R.packed_attn_ref(*(np64(t) for t in (q, k, v)), cu, 0.125)
     assert (np.abs(np64(lse) - rl) <= 1e-6 * np.abs(rl)).all()
     assert (np.abs(np64(out) - ref) <= 1.1 * U * (mag + np.abs(ref)) + 2e-5 * mag).all()
+
+
+@pytest.mark.parametrize("T,r", [(300000, 1), (1 << 20, 2)])
+def test_very_many_tokens_of_short_sequences(B, T, r):
+    """sequences that repeat every 12800 tokens: gradients repeat to the bit, and are those of one call of 12800"""
+    import torch
+    n = 12800
+    lens = [100, 1, 0, 37, 62] * 64
+    assert sum(lens) == n
+    q, k, v, dout = inputs(n, r, 1, 64, seed=3)
+    cu = np.concatenate([[0], np.cumsum(lens)])
+    ref = run(B, q, k, v, dout, cu.tolist(), 0.125)
+    times = -(-T // n)
+    many = np.concatenate([[0]] + [cu[1:] + n * i for i in range(times)])
+    big = [t.repeat(times, 1, 1)[:T] for t in (q, k, v, dout)]
+    got = run(B, *big, np.minimum(many, T).tolist(), 0.125)
+    whole = T // n * n
+    for g, c in zip((got[0], *got[2:]), (ref[0], *ref[2:])):
+        assert torch.equal(g[:whole].view(-1, *c.shape), c.expand(T // n, *c.shape))
