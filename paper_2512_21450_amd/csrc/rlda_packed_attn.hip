@@ -1264,13 +1264,17 @@ int check_backward(const rl_packed_attn_backward_desc* d) {
 }
 int64_t key_blocks(int64_t T) { return (T + KEY_BLOCK - 1) / KEY_BLOCK; }
 // Workgroups to a block of keys, each of 512 rows and more: as many as find places at once where blocks are few (us without / with: 8 sequences of 64 to 452 tokens of
-// 16/2 heads of 128 columns 71 / 38, 1100 of 28/4 109 / 53, 4 x 1024 of 14/2 of 64 columns 68 / 46); two where blocks of long sequences, the first of which have twice the
-// rows of an average one, are too few to even out (4000 of 28/4 405 / 293, 3 x 1000 to 2000 237 / 185, 6000 670 / 621; 7500, 472 blocks, 861 / 887; 30 x 100 to 300,
-// 376 blocks of some 1400 rows a sequence, 58 / 86).
+// 16/2 heads of 128 columns 71 / 38, 1100 of 28/4 109 / 53, 4 x 1024 of 14/2 of 64 columns 68 / 46); two where blocks of long sequences are some 1.5 to a compute
+// unit.  What two have to gain there is half of the longest block's time, what they cost is their sums, written and read again: so many rows for each block, fewer
+// where there are several sequences, whose lengths may differ (gradient of so many blocks and mean rows a sequence of 128 columns, one / two.  One sequence: 264,
+// 4224 152 / 161, 264, 8448 272 / 258, 392, 6272 216 / 236, 392, 43904 1029 / 989.  Two to five: 264, 2112 103 / 111, 392, 2508 136 / 156, 392, 4181 187 / 201, 330, 5280
+// 215 / 206, 392, 8780 313 / 290.  Eight and more, lengths alike: 264, 2464 101 / 113, 392, 3658 142 / 171, 264, 5913 181 / 167; up to twice the mean: 264, 2464 155 / 132,
+// 392, 3658 228 / 207.  64 columns lie alike.  Above: 460, 17173 524 / 529 and 559 / 539.)
 int splits_for(int64_t T, int S, int Hq, int Hkv) {
   const int64_t blocks = key_blocks(T) * Hkv, rows = T * (Hq / Hkv) / (S > 0 ? S : 1);
   int64_t s = 256 / blocks;
-  if (s < 2 && blocks < 400 && rows >= 2048) s = 2;
+  const int64_t least = S <= 1 ? 32 * blocks : S < 8 ? 10 * blocks : 2048;
+  if (s < 2 && blocks < 400 && rows >= least) s = 2;
   if (s > rows / 512) s = rows / 512;
   return (int)(s < 1 ? 1 : s > 8 ? 8 : s);
 }

@@ -25,3 +25,12 @@ def test_packed_attn_backward_grid_of_key_blocks():
 def test_scales_whose_base_2_form_is_no_number(scale):
     assert B.rl_packed_attn_raw(attn(scale=scale)) == -1 and B.rl_packed_attn_backward_raw(attn_grad(scale=scale)) == -1
     assert B.rl_packed_attn_backward_workspace_bytes(attn_grad(scale=scale)) == 0
+
+
+@pytest.mark.parametrize("T,S,Hq,Hkv,d,parts", [(3136, 1, 8, 8, 64, 1), (3136, 3, 16, 8, 128, 1), (6272, 1, 4, 4, 128, 1), (8448, 1, 2, 2, 128, 2), (4000, 1, 28, 4, 128, 2),
+                                                (6272, 16, 28, 4, 128, 2), (1100, 1, 28, 4, 128, 3), (7040, 1, 28, 4, 128, 1)])
+def test_packed_attn_workgroups_that_share_a_block_of_keys(T, S, Hq, Hkv, d, parts):
+    """only where their sums, which the workspace holds, are worth writing: one sequence of few rows for so many blocks gains nothing by it"""
+    plain = T * Hq * 8 + (T + 63) // 64 * 8
+    need = B.rl_packed_attn_backward_workspace_bytes(B.make_packed_attn_backward_desc(T, S, Hq, Hkv, d, 0.1))
+    assert need == plain if parts == 1 else need == (plain + 255) // 256 * 256 + parts * 2 * T * Hkv * d * 4
