@@ -10,7 +10,7 @@
 //   dhidden    m = hidden, k = vocabulary of the piece: weight rows are read transposed from LDS; few output tiles, so k
 //              is cut into splits with sums of their own (fp32), which a last kernel adds in order
 //   dweight    m = hidden, n = vocabulary, k = tokens: both operands transposed
-// Scratch is zero where a token or a column does not exist, so that no product needs a mask.
+// Scratch is zero where a token or a column does not exist, and so is, in LDS, what a tile of weights has behind its last column or row: no product needs a mask.
 //
 // Weights that mask a token are infinite or NaN, and its dz, which is 0, would make NaN of them in dhidden.  A logit that is not finite says that there may
 // be some (hidden states that add anything are finite, unless they mask their row's every logit): the recomputation then raises a flag, and dhidden's
@@ -20,8 +20,8 @@
 // few they need not (2 tokens: dweight 2.4e-3 of its norm off against 1.6e-3).  Up to 32 tokens, whose tiles of 64 are half empty, the second half
 // holds what the first one's rounding left over: the products take it along as tokens of their own.
 //
-// Measured: 4096 tokens x 3584 x 151936 forward 3.85 ms (1.16 Pflop/s, 82 % of the library's bare product); 2048 tokens with gradient 8.25 ms: forward
-// 1.95, recompute 2.2, dhidden 2.0, dweight 1.9; 333 x 896 x 50001 forward 47 us, recompute 50, dhidden 40, dweight 44; 16 x 2048 x 151936, the weights at 4.4 to 5.5 TB/s:
+// Measured: 4096 tokens x 3584 x 151936 forward 3.83 ms (1.16 Pflop/s, 82 % of the library's bare product); 2048 tokens with gradient 8.18 ms: forward
+// 1.96, recompute 2.2, dhidden 2.0, dweight 1.9; 333 x 896 x 50001 forward 44 us, recompute 50, dhidden 40, dweight 44; 16 x 2048 x 151936, the weights at 4.4 to 5.5 TB/s:
 // 114, 140, 113, 125.
 #include <hip/hip_runtime.h>
 #include <stddef.h>

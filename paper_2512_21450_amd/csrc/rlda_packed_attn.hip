@@ -18,11 +18,13 @@
 //             so heads of a group add up in its registers, in a fixed order, without atomics (the price: S and dP are computed twice).
 //             P and dS are rounded for the last two; keys that few rows see also take the products of what that left over
 //             (6 sequences of 2 tokens: dk off by 2.55e-3 of its norm, the rounding of the result alone is 1.66e-3)
+// Roundings to bf16: P in front of V (out off by 1.9e-3 to 2.1e-3 of its norm), P and dS in the gradients (2.4e-3 in all); two parts of 8 bits each would double a
+// product's cost, and are taken where few terms make up a sum.
 // Tiles of 64 keys or rows move straight into LDS, two buffers.  Their pattern (xor on a row's 16-byte chunks) lets both the 16-byte reads (16
 // rows at one column) and the transposing 8-byte reads (4 rows of 64 bytes) meet no bank conflict.
 //
-// Measured, 28/4 heads of 128 columns: forward of 8192 tokens 466 us (1.03 Pflop/s), of 10 sequences of 1280 to 1996 245, their dq 350 (0.83 Pflop/s
-// over its three products), dk and dv 505 (0.77 over four), at 1.7 GHz with the matrix cores busy 46 to 50 % of the cycles; 14/2 heads of 64, 48 sequences of 24 to 340: 19, 31, 38.
+// Measured, 28/4 heads of 128 columns: forward of 8192 tokens 453 us (1.06 Pflop/s), of 10 sequences of 1280 to 1996 240, their dq 350 (0.83 Pflop/s
+// over its three products), dk and dv 490 (0.79 over four), at 1.7 GHz with the matrix cores busy 46 to 50 % of the cycles; 14/2 heads of 64, 48 sequences of 24 to 340: 19, 33, 42.
 //
 // A masked weight is 0, but 0 times infinity is not: whatever a key outside a row's range holds would reach the row through a
 // product.  It cannot do so unseen, sums are then not finite; such rows (or keys) are computed again, with zeros in place of what is no number.

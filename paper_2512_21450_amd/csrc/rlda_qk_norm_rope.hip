@@ -9,7 +9,9 @@
 // The next head's loads are issued before the present one's arithmetic.  Stores go past the caches, and so do loads of calls
 // that read more than the last-level cache holds (smaller ones may find there what a projection has just left).  us, inputs
 // changing, all through the caches / stores past them / loads too / by this rule: 40960 tokens of 28/4 heads of 128 bf16 forward
-// 126.6 / 123.5 / 119.9 / 119.9 (5.6 TB/s), 16384 forward and backward 139.6 / 122.9 / 131.3 / 121.0.
+// 126.6 / 123.5 / 119.9 / 119.9 (5.6 TB/s), 16384 forward and backward 139.6 / 122.9 / 131.3 / 121.0.  A consumer finds less in the caches then: the forward call and
+// attention over its outputs, in a graph, stores through / past the caches 9.9 / 10.4 (64 tokens of 28/4 heads of 128), 45.2 / 47.5 (4096), 142 / 146 (16384), 14.9 / 15.1
+// (2048 of 14/2 of 64), 29.4 / 29.1 (8192), the forward call alone 14.7 / 12.3 (4096 of 28/4).
 //
 // Backward, a lane also sums g x rs of its elements over all heads it meets; lanes, wavefronts and then workgroups are added
 // in a fixed order (the last by a second kernel, in fp64).

@@ -3,9 +3,9 @@
 // An operand is a matrix of rows and columns in memory whose contraction index k runs along its columns (K_COLS: the rows are
 // m or n) or along its rows (K_ROWS: the columns are m or n).  Tiles of BK k move from memory straight into LDS (16 bytes a
 // lane, a wavefront's 1 KB lands contiguously) into a ring of STAGES buffers, all but one ahead of the products.  Tiles of 256 take two of 64 k:
-// four of 32 k, lines of 64 bytes, made 4096 x 151936 x 3584 5 % slower (4.07 ms, 4.30 so), as did fragments asked for a step ahead (4.07),
-// wavefronts of a SIMD that fetch and multiply in turns between barriers (4.05 to 4.2) and one wavefront a SIMD with 128 x 128 (4.6);
-// the card holds 1.65 GHz at 65 % of the matrix unit's cycles under this load.  Tiles of few rows, whose loads are all there is to do,
+// four of 32 k, lines of 64 bytes, made 4096 x 151936 x 3584 5 % slower (4.07 -> 4.30 ms); fragments asked for a step ahead (4.07) and
+// wavefronts of a SIMD that fetch and multiply in turns between barriers (4.05 to 4.2) gained nothing, one wavefront a SIMD with 128 x 128 lost (4.6);
+// the forward call's product takes 3.8 ms now, and the card holds 1.65 GHz at 59 % of the matrix unit's cycles under this load.  Tiles of few rows, whose loads are all there is to do,
 // take four buffers (16 x 151936 x 2048: 137 us with two, 118 with four, 130 with eight).  The
 // layout's xor pattern, under which fragment reads meet no bank conflict, is applied to the lane's address in memory: K_COLS fragments are read with
 // 16-byte reads (16 rows at one column must differ), K_ROWS fragments with the transposing 8-byte reads (4 rows of 64 bytes each).
