@@ -14,7 +14,8 @@
 //
 // Weights that mask a token are infinite or NaN, and its dz, which is 0, would make NaN of them in dhidden.  A logit that is not finite says that there may
 // be some (hidden states that add anything are finite, unless they mask their row's every logit): the recomputation then raises a flag, and dhidden's
-// product reads the weights' infinities and NaN as zeros.  Only a masked token that was sampled has a dz; its infinities are added at the end.
+// product reads the weights' infinities and NaN as zeros (50 NaN rows: recompute and dhidden of 2048 x 3584 x 151936 4.19 -> 4.53 ms, 333 x 896 x 50001 108 -> 135 us).
+// Only a masked token that was sampled has a dz; its infinities are added at the end.
 //
 // dz rounded to bf16 is off by the roundings of its few large elements; over many tokens they average out beside the result's own, over a
 // few they need not (2 tokens: dweight 2.4e-3 of its norm off against 1.6e-3).  Up to 32 tokens, whose tiles of 64 are half empty, the second half
